@@ -241,6 +241,131 @@ int saf_calib_accumulate(saf_ctx* ctx, const saf_problem* problem, const void* Q
 int saf_calib_finalize(saf_ctx* ctx, int32_t H, int32_t T, int64_t n_total, float* mean_inout, const double* sumsq,
                        const double* sum_plogp, double* s_var_out, double* s_kl_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Rotary positions.  The layer calls take queries and keys to which the caller has applied its position encoding; these calls
+ * apply the rotary one, and carry the gradients back through it.  The pair i of the first `rot_dim` features of a head, (x[2i],
+ * x[2i+1]) if `interleaved`, else (x[i], x[i + rot_dim/2]), is turned by the angle t = position * freqs[i]:
+ *     (a, b) -> mscale * (a cos t - b sin t, b cos t + a sin t);
+ * the other features are copied.  Angles are reduced in fp64, so that far positions lose nothing; products are fp32, rounded
+ * once on the way out. */
+typedef struct {
+  int32_t B, T;                /* tokens [B][T]; >= 1 */
+  int32_t Hq, Hk;              /* heads of the first and of the second tensor (queries and keys, or their gradients); either may
+                                  be 0, the pointers of an absent tensor are not read */
+  int32_t D;                   /* head dimension, a multiple of 8, up to 512 */
+  int32_t rot_dim;             /* even, 0 .. D */
+  int32_t interleaved;
+  int32_t in_dtype, out_dtype; /* SAF_BF16 or SAF_F32 each */
+  float mscale;                /* factor on the turned features (1: none) */
+  int64_t q_strides[3], k_strides[3];    /* inputs, elements: batch, head, token; multiples of 8, as all strides here */
+  int64_t qo_strides[3], ko_strides[3];  /* outputs */
+} saf_rotary;
+
+/* Frequencies of rotary positions, host only: freqs_out (host double [rot_dim/2]) = radians per position, *mscale_out (may be
+ * NULL) = the factor for saf_rotary.mscale.  With f_i = base^(-2i/rot_dim):
+ *   SAF_ROPE_PLAIN   f_i
+ *   SAF_ROPE_LINEAR  f_i / factor                                   (positions compressed into the trained context)
+ *   SAF_ROPE_BASE    f_i with base * factor^(rot_dim/(rot_dim-2))   (the slowest pair stretched by `factor`, the fastest kept;
+ *                    rot_dim > 2)
+ *   SAF_ROPE_RAMP    pairs of more than 32 turns over `trained_len` positions keep f_i, pairs of less than 1 get f_i / factor, a
+ *                    linear ramp over the pair's index between (rounded outwards); mscale = 0.1 ln(factor) + 1 (the method
+ *                    published as YaRN)
+ * rot_dim even, >= 2; base > 1; factor >= 1; trained_len >= 1 (SAF_ROPE_RAMP only). */
+enum { SAF_ROPE_PLAIN = 0, SAF_ROPE_LINEAR = 1, SAF_ROPE_BASE = 2, SAF_ROPE_RAMP = 3 };
+int saf_rotary_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len, double* freqs_out,
+                     float* mscale_out);
+
+/* q_out, k_out <- q, k turned forward.  positions: device int32 [B][T], or NULL for 0 .. T-1 in every batch entry; freqs: device
+ * double [rot_dim/2].  An output may be its input (same address, strides and dtype); otherwise they must not overlap. */
+int saf_rotary_fwd(saf_ctx* ctx, const saf_rotary* r, const void* q, const void* k, const int32_t* positions, const double* freqs,
+                   void* q_out, void* k_out, void* stream);
+
+/* The gradients' way back: dq, dk <- dq_out, dk_out (gradients of saf_rotary_fwd's outputs: dQ and dK of saf_hybrid_attn_bwd, fp32
+ * or bf16) turned backward by the same angles and scaled by the same mscale.  r->q_strides, k_strides and in_dtype describe
+ * dq_out and dk_out, r->qo_strides, ko_strides and out_dtype dq and dk. */
+int saf_rotary_bwd(saf_ctx* ctx, const saf_rotary* r, const void* dq_out, const void* dk_out, const int32_t* positions,
+                   const double* freqs, void* dq, void* dk, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Serving from a paged cache.  Keys and values of one layer live in pools of pages, [n_pages][heads][page_size][D] bf16 through
+ * element strides; token t of request r lies in slot t % page_size of page block_table[r][t / page_size].  A step brings each of
+ * R requests some new tokens, whose rows are packed request after request into arrays of N rows.  A step is:
+ *   saf_cache_plan    once: pages for the new tokens, and what the layers need to know
+ *   saf_cache_append  per layer: queries and keys rotated, keys and values written into the pools
+ *   saf_cache_attn    per layer: attention of the new tokens over their requests' caches
+ * Lengths, tables and plans are device arrays, so a recorded step serves steps of other lengths within R, N, max_len, max_new. */
+typedef struct {
+  int32_t R;                   /* requests; 1 .. 4096 */
+  int32_t N;                   /* rows of the packed arrays; >= 1.  Rows behind the last request's are left as they are. */
+  int32_t page_size, n_pages;  /* slots of a page (saf_cache_attn: a multiple of 16), pages of a pool; product < 2^31 */
+  int32_t max_pages;           /* row length of block_table; R * max_pages < 2^31 */
+  int32_t H, kv_group, D;      /* query heads, query heads per cached head (0 or 1: one), head dimension; as in saf_problem */
+  int32_t Tp;                  /* row length of alpha and rho; >= max_len where heads are frozen */
+  int32_t max_len;             /* saf_cache_attn: no request's cache holds more tokens, new ones included; <= max_pages * page_size */
+  int32_t max_new;             /* saf_cache_attn: no request brings more new tokens; 1 .. 64 */
+  int32_t o_dtype;             /* of O: SAF_BF16 or SAF_F32 */
+  float softmax_scale;         /* <= 0 selects 1/sqrt(D) */
+  int32_t reserved;            /* 0 */
+  int64_t q_strides[2], o_strides[2];    /* elements: row, head */
+  int64_t vn_strides[2];                 /* saf_cache_append: the new values, row, head */
+  int64_t k_strides[3], v_strides[3];    /* the pools: page, head, slot */
+} saf_cache;
+
+/* Plan of a step: the pages a request holds follow its length, and the packed arrays are described.  All pointers are device
+ * int32 arrays unless said otherwise; c: R, N, page_size, n_pages, max_pages.
+ *   ctx_lens, new_lens [R]  tokens in the cache before the step, and new ones (0 and 0: an idle or finished request)
+ *   parents [N] or NULL     drafted trees: place of the token that a new token follows among its request's new tokens, before its
+ *                           own, or -1 for the last cached one (any other value counts as -1); at most 64 new tokens a request
+ *   held_in, held_out [R]   pages of each request before and after (may be the same array)
+ *   free_count_in, _out [1] entries of free_list before and after (may be the same)
+ *   free_list [n_pages]     stack of free pages, top last; block_table [R][max_pages]
+ * A request keeps need = ceil((ctx + new) / page_size) pages.  First the pages beyond it are pushed onto the free stack, in order of
+ * requests and places; then requests that hold too few pop theirs in order.  A request whose turn finds too few left gets
+ * none, nor does any behind it that needs some: it keeps what it held, missing = the pages it asked for, no slots, kv_lens 0.
+ * A request that cannot be served as given (more than max_pages pages, rows beyond N, a negative length, more than 64 new tokens in a
+ * tree) likewise, with missing = -1.  Table entries behind a request's pages and stack entries from free_count_out on are left as they are.
+ *   new_offsets [R+1]       first row of each request (at most N); kv_lens [R] ctx + new, or 0; missing [R] 0 when served
+ *   slots [N]               page * page_size + slot of the row's token, or -1 (not served; rows behind the last request)
+ *   positions [N]           ctx + place, in a tree ctx + depth; 0 behind the last request
+ *   tree_masks uint64 [N]   (with parents; else NULL) bit j: the row's token sees its request's new token j: itself and its ancestors
+ * Outputs must not overlap inputs but where said.  Not served requests have rows all the same: saf_cache_append skips them,
+ * saf_cache_attn gives zeros. */
+int saf_cache_plan(saf_ctx* ctx, const saf_cache* c, const int32_t* ctx_lens, const int32_t* new_lens, const int32_t* parents,
+                   const int32_t* held_in, int32_t* held_out, const int32_t* free_count_in, int32_t* free_count_out,
+                   int32_t* free_list, int32_t* block_table, int32_t* new_offsets, int32_t* kv_lens, int32_t* slots,
+                   int32_t* positions, uint64_t* tree_masks, int32_t* missing, void* stream);
+
+/* New tokens of one layer: q_out <- q and the key pool <- k, both turned as by saf_rotary_fwd, the value pool <- v.
+ *   r: B = 1, T = c->N, Hq (0: no queries; q and q_out are not touched), Hk = the pools' heads, D = c->D, rot_dim (0: keys and
+ *      queries as they are), both dtypes SAF_BF16; q_strides, k_strides, qo_strides (batch strides are not used).
+ *   v: bf16 rows by c->vn_strides; c: N, page_size, n_pages, H, kv_group, D, k_strides, v_strides, vn_strides.
+ *   slots, positions [N] as from saf_cache_plan (positions may be NULL if rot_dim is 0).  A row whose slot lies outside the pools (-1)
+ *      is skipped, its q_out row too.  Slots of one call must differ from each other. */
+int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, const void* q, const void* k, const void* v,
+                     const int32_t* slots, const int32_t* positions, const double* freqs, void* q_out, void* k_cache,
+                     void* v_cache, void* stream);
+
+/* Attention of a step's new tokens over the cache, in which their own keys and values already lie.  A request with n new tokens and
+ * kv_len cached ones (new ones included, ctx = kv_len - n) has keys j in [0, kv_len).  Its new token i sees those with j < ctx, and
+ * of the new ones those whose bit j - ctx is set in tree_masks, or, with tree_masks NULL, those up to itself.
+ *   ordinary head   O = softmax(scale q K^T) V over the keys seen
+ *   frozen head     O = sum_j w_j V_j / sum_j w_j over the keys seen, w_j = exp(alpha[h][p_j] + rho[h][p - p_j]), p_j = j for j < ctx and
+ *                   the new token's position otherwise, p the row's own (keys with p_j > p count as not seen).  Where the keys seen hold each position
+ *                   0..p once (a chain; a tree's ancestors), that is P^ V of Eq. "compact-prior" with its own Z(p).
+ * A row that sees nothing gives zeros.  NaN and infinities in slots that a row does not see do not reach it.
+ *   Q, O: [N][H][D] by c->q_strides, o_strides; K and V pools; block_table, new_offsets, kv_lens as from saf_cache_plan (lengths beyond
+ *   max_len and page numbers outside the pool are clamped, rows beyond max_new of a request are left as they are)
+ *   positions [N] of the new tokens, or NULL: ctx + place (read for frozen heads only; values outside [0, Tp) are clamped)
+ *   frozen_mask_host, alpha, rho as in saf_hybrid_attn_fwd (no logZ: the sum over the keys is formed here); H <= 1024
+ *   LSE: device fp32 [N][H] or NULL: natural-log sum of exp of the scaled scores, 0 for frozen heads, -inf for a row of an
+ *   ordinary head that sees nothing
+ * Q rows of frozen heads are never read, nor keys where all heads of a group are frozen.  D in {64, 96, 128}.  Results do not vary from run to run.  One launch;
+ * recordable after one warm-up call with the same R, H, kv_group, D and max_new or larger ones. */
+int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* k_cache, const void* v_cache,
+                   const int32_t* block_table, const int32_t* new_offsets, const int32_t* kv_lens, const int32_t* positions,
+                   const uint64_t* tree_masks, const uint8_t* frozen_mask_host, const float* alpha, const float* rho, void* O,
+                   float* LSE, void* stream);
+
 /* Device-side status of the most recent launches on this context: SAF_OK or SAF_ERR_DEVICE_TIMEOUT.
  * Synchronises the context's device status word with the host (blocks until the stream used by the
  * last call has drained).  `detail_out` (may be NULL) receives the raw word: site and CTA that gave up. */
@@ -262,7 +387,9 @@ enum {
   SAF_KERNEL_FIT_MARGINALS = 8,/* target marginals (saf_fit_marginals) */
   SAF_KERNEL_CALIB = 9,        /* calibration statistics kernel (saf_calib_accumulate) */
   SAF_KERNEL_CALIB_FINALIZE = 10, /* mean and scores (saf_calib_finalize) */
-  SAF_KERNEL_COUNT = 11
+  SAF_KERNEL_ROTARY = 11,      /* saf_rotary_fwd, saf_rotary_bwd */
+  SAF_KERNEL_CACHE_PLAN = 12, SAF_KERNEL_CACHE_APPEND = 13, SAF_KERNEL_CACHE_ATTN = 14, /* the three calls of a cached step */
+  SAF_KERNEL_COUNT = 15
 };
 int saf_set_profiling(saf_ctx* ctx, int32_t enable);
 int saf_get_kernel_time(saf_ctx* ctx, int32_t which, float* total_ms_out, int32_t* launches_out);

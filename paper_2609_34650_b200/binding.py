@@ -19,6 +19,8 @@ SAF_ERR_INVALID_ARG, SAF_ERR_UNSUPPORTED, SAF_ERR_CUDA, SAF_ERR_DEVICE_TIMEOUT, 
 SAF_BF16, SAF_F32 = 0, 1
 SAF_KERNEL_FWD, SAF_KERNEL_BWD, SAF_KERNEL_BWD_PREP, SAF_KERNEL_BWD_FINALIZE, SAF_KERNEL_LOGZ, SAF_KERNEL_SCALE = range(6)
 SAF_KERNEL_PGRAD, SAF_KERNEL_FIT, SAF_KERNEL_FIT_MARGINALS, SAF_KERNEL_CALIB, SAF_KERNEL_CALIB_FINALIZE = 6, 7, 8, 9, 10
+SAF_KERNEL_ROTARY, SAF_KERNEL_CACHE_PLAN, SAF_KERNEL_CACHE_APPEND, SAF_KERNEL_CACHE_ATTN = range(11, 15)
+SAF_ROPE_PLAIN, SAF_ROPE_LINEAR, SAF_ROPE_BASE, SAF_ROPE_RAMP = range(4)
 
 
 class SafProblem(C.Structure):
@@ -27,6 +29,20 @@ class SafProblem(C.Structure):
                 ("packed_qk", C.c_int32), ("o_dtype", C.c_int32),
                 ("q_strides", C.c_int64 * 3), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3),
                 ("o_strides", C.c_int64 * 3)]
+
+
+class SafRotary(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("D", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("in_dtype", C.c_int32), ("out_dtype", C.c_int32), ("mscale", C.c_float),
+                ("q_strides", C.c_int64 * 3), ("k_strides", C.c_int64 * 3), ("qo_strides", C.c_int64 * 3), ("ko_strides", C.c_int64 * 3)]
+
+
+class SafCache(C.Structure):
+    _fields_ = [("R", C.c_int32), ("N", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("H", C.c_int32), ("kv_group", C.c_int32), ("D", C.c_int32), ("Tp", C.c_int32), ("max_len", C.c_int32),
+                ("max_new", C.c_int32), ("o_dtype", C.c_int32), ("softmax_scale", C.c_float), ("reserved", C.c_int32),
+                ("q_strides", C.c_int64 * 2), ("o_strides", C.c_int64 * 2), ("vn_strides", C.c_int64 * 2),
+                ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3)]
 
 
 class SafError(RuntimeError):
@@ -69,11 +85,19 @@ def load_library() -> C.CDLL:
     lib.saf_pattern_logz_static.restype = C.c_int
     lib.saf_fit_handover.argtypes = [vp, i32, C.POINTER(i32)]
     lib.saf_fit_math.argtypes = [i32, i32, i32, vp, vp, vp]
+    pr, pc, dp = C.POINTER(SafRotary), C.POINTER(SafCache), C.POINTER(C.c_double)
+    lib.saf_rotary_freqs.argtypes = [i32, C.c_double, i32, C.c_double, i32, dp, C.POINTER(C.c_float)]
+    lib.saf_rotary_fwd.argtypes = [vp, pr, vp, vp, vp, vp, vp, vp, vp]
+    lib.saf_rotary_bwd.argtypes = [vp, pr, vp, vp, vp, vp, vp, vp, vp]
+    lib.saf_cache_plan.argtypes = [vp, pc] + [vp] * 16
+    lib.saf_cache_append.argtypes = [vp, pc, pr] + [vp] * 10
+    lib.saf_cache_attn.argtypes = [vp, pc] + [vp] * 8 + [u8p] + [vp] * 5
     lib.saf_build_worklist.argtypes = [i32, i32, i32, u8p, i32, i32, i32, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
     for name in ("saf_create", "saf_destroy", "saf_pattern_prepare", "saf_hybrid_attn_fwd", "saf_hybrid_attn_bwd",
                  "saf_hybrid_attn_step_host", "saf_last_device_status", "saf_build_worklist", "saf_set_profiling",
                  "saf_get_kernel_time", "saf_pattern_grad", "saf_fit_marginals", "saf_fit_compact", "saf_calib_accumulate", "saf_calib_finalize", "saf_fit_handover",
-                 "saf_fit_math"):
+                 "saf_fit_math", "saf_rotary_freqs", "saf_rotary_fwd", "saf_rotary_bwd", "saf_cache_plan", "saf_cache_append",
+                 "saf_cache_attn"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -157,6 +181,69 @@ def make_problem(q_like, Tp, softmax_scale=0.0, grad_dtype=SAF_F32, k_like=None,
     return p
 
 
+def _dtype(t):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise SafError(SAF_ERR_UNSUPPORTED, f"dtype {t.dtype}")
+    return SAF_F32 if t.dtype == torch.float32 else SAF_BF16
+
+
+def make_rotary(q, k, q_out, k_out, rot_dim, interleaved=False, mscale=1.0):
+    """saf_rotary from [B,H,T,D] tensors (any strides with a unit feature stride), or [N,H,D] ones: packed rows, one batch entry.
+    q or k (with its output) may be None, and k_out where the keys go into a cache; for saf_rotary_bwd pass the gradients."""
+    first = q if q is not None else k
+    r = SafRotary()
+    packed = first.dim() == 3
+    r.B, r.T, r.D = (1, first.shape[0], first.shape[2]) if packed else (first.shape[0], first.shape[2], first.shape[3])
+    r.Hq, r.Hk = (0 if t is None else t.shape[1] for t in (q, k))
+    r.rot_dim, r.interleaved, r.mscale = rot_dim, int(interleaved), mscale
+    r.in_dtype = _dtype(first)
+    out = q_out if q_out is not None else k_out
+    r.out_dtype = r.in_dtype if out is None else _dtype(out)
+    for name, t, like in (("q_strides", q, q), ("k_strides", k, k), ("qo_strides", q_out, q), ("ko_strides", k_out, k)):
+        if t is None:
+            continue
+        assert t.stride(-1) == 1, "feature stride must be 1"
+        assert t.shape == like.shape and t.shape[-1] == r.D and t.dim() == first.dim(), "outputs have their inputs' shapes"
+        assert _dtype(t) == (r.in_dtype if name[1] == "_" else r.out_dtype), "one dtype for both inputs, one for both outputs"
+        arr = getattr(r, name)
+        arr[0], arr[1], arr[2] = (t.shape[0] * t.stride(0), t.stride(1), t.stride(0)) if packed else (t.stride(0), t.stride(1), t.stride(2))
+    return r
+
+
+def make_cache(R, N, page_size, n_pages, max_pages, k_cache=None, v_cache=None, q_like=None, o_like=None, v_like=None, Tp=0,
+               max_len=0, max_new=1, softmax_scale=0.0):
+    """saf_cache from its sizes and, as far as a call uses them, the pools [n_pages,heads,page_size,D], queries and outputs [N,H,D]
+    and new values [N,heads,D] (any strides with a unit feature stride)."""
+    c = SafCache()
+    c.R, c.N, c.page_size, c.n_pages, c.max_pages = R, N, page_size, n_pages, max_pages
+    c.Tp, c.max_len, c.max_new, c.softmax_scale = Tp, max_len, max_new, softmax_scale
+    c.kv_group = 1
+    for name, t in (("k_strides", k_cache), ("v_strides", v_cache)):
+        if t is not None:
+            assert t.stride(3) == 1 and t.shape[0] == n_pages and t.shape[2] == page_size, "pools are [n_pages,heads,page_size,D]"
+            c.H, c.D = t.shape[1], t.shape[3]
+            getattr(c, name)[:] = [t.stride(0), t.stride(1), t.stride(2)]
+    for name, t in (("q_strides", q_like), ("o_strides", o_like), ("vn_strides", v_like)):
+        if t is not None:
+            assert t.stride(2) == 1 and t.shape[0] == N and t.shape[2] == c.D, "packed rows are [N,heads,D]"
+            getattr(c, name)[:] = [t.stride(0), t.stride(1)]
+    if q_like is not None:
+        c.kv_group = q_like.shape[1] // c.H
+        c.H = q_like.shape[1]
+    if o_like is not None:
+        c.o_dtype = _dtype(o_like)
+    return c
+
+
+def saf_rotary_freqs(rot_dim, base=10000.0, scaling=SAF_ROPE_PLAIN, factor=1.0, trained_len=0):
+    """Host only: (radians per position, float64 [rot_dim/2]; factor for make_rotary's mscale)."""
+    freqs, mscale = np.zeros(max(rot_dim // 2, 1), dtype=np.float64), C.c_float(1.0)
+    _check(load_library().saf_rotary_freqs(rot_dim, float(base), int(scaling), float(factor), int(trained_len),
+                                           freqs.ctypes.data_as(C.POINTER(C.c_double)), C.byref(mscale)), "saf_rotary_freqs")
+    return freqs, mscale.value
+
+
 def saf_fit_math(device, which, x, y):
     """y = 1 / x (which = 0), sqrt(x) (1) or exp(x) (2) by the fitter's own fp64 functions."""
     _check(load_library().saf_fit_math(device, which, x.numel(), _ptr(x), _ptr(y), _stream()), "saf_fit_math")
@@ -230,6 +317,32 @@ class Context:
         _check(self._lib.saf_hybrid_attn_step_host(self._h, C.byref(prob), _ptr(Q), _ptr(K), _ptr(V), _ptr(dO), _mask(mask),
                                                    _ptr(alpha), _ptr(rho), int(prepare), _ptr(O), _ptr(LSE), _ptr(dQ),
                                                    _ptr(dK), _ptr(dV)), "saf_hybrid_attn_step_host")
+
+    def saf_rotary_fwd(self, rot, q, k, positions, freqs, q_out, k_out):
+        _check(self._lib.saf_rotary_fwd(self._h, C.byref(rot), _ptr(q), _ptr(k), _ptr(positions), _ptr(freqs), _ptr(q_out),
+                                        _ptr(k_out), _stream()), "saf_rotary_fwd")
+
+    def saf_rotary_bwd(self, rot, dq_out, dk_out, positions, freqs, dq, dk):
+        _check(self._lib.saf_rotary_bwd(self._h, C.byref(rot), _ptr(dq_out), _ptr(dk_out), _ptr(positions), _ptr(freqs), _ptr(dq),
+                                        _ptr(dk), _stream()), "saf_rotary_bwd")
+
+    def saf_cache_plan(self, cache, ctx_lens, new_lens, parents, held_in, held_out, free_count_in, free_count_out, free_list,
+                       block_table, new_offsets, kv_lens, slots, positions, tree_masks, missing):
+        _check(self._lib.saf_cache_plan(self._h, C.byref(cache), _ptr(ctx_lens), _ptr(new_lens), _ptr(parents), _ptr(held_in),
+                                        _ptr(held_out), _ptr(free_count_in), _ptr(free_count_out), _ptr(free_list),
+                                        _ptr(block_table), _ptr(new_offsets), _ptr(kv_lens), _ptr(slots), _ptr(positions),
+                                        _ptr(tree_masks), _ptr(missing), _stream()), "saf_cache_plan")
+
+    def saf_cache_append(self, cache, rot, q, k, v, slots, positions, freqs, q_out, k_cache, v_cache):
+        _check(self._lib.saf_cache_append(self._h, C.byref(cache), C.byref(rot), _ptr(q), _ptr(k), _ptr(v), _ptr(slots),
+                                          _ptr(positions), _ptr(freqs), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream()),
+               "saf_cache_append")
+
+    def saf_cache_attn(self, cache, Q, k_cache, v_cache, block_table, new_offsets, kv_lens, positions, tree_masks, mask, alpha, rho,
+                       O, LSE):
+        _check(self._lib.saf_cache_attn(self._h, C.byref(cache), _ptr(Q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+                                        _ptr(new_offsets), _ptr(kv_lens), _ptr(positions), _ptr(tree_masks), _mask(mask),
+                                        _ptr(alpha), _ptr(rho), _ptr(O), _ptr(LSE), _stream()), "saf_cache_attn")
 
     def saf_set_profiling(self, enable: bool):
         _check(self._lib.saf_set_profiling(self._h, int(enable)), "saf_set_profiling")

@@ -1493,6 +1493,229 @@ int saf_calib_finalize(saf_ctx* ctx, int32_t H, int32_t T, int64_t n_total, floa
   return SAF_OK;
 }
 
+// ---------------------------------------------------------------------------------------------- rotary positions, paged cache
+
+int saf_rotary_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len, double* freqs_out,
+                     float* mscale_out) {
+  if (!freqs_out || rot_dim < 2 || rot_dim % 2 != 0 || !(base > 1.0) || !(factor >= 1.0) || !std::isfinite(base) ||
+      !std::isfinite(factor) || scaling < SAF_ROPE_PLAIN || scaling > SAF_ROPE_RAMP)
+    return SAF_ERR_INVALID_ARG;
+  if ((scaling == SAF_ROPE_RAMP && trained_len < 1) || (scaling == SAF_ROPE_BASE && rot_dim == 2)) return SAF_ERR_INVALID_ARG;
+  if (scaling == SAF_ROPE_BASE) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+  // (fractional) index of the pair that makes `turns` turns over the trained length
+  auto pair = [&](double turns) {
+    return rot_dim * std::log(trained_len / (turns * 6.283185307179586)) / (2.0 * std::log(base));
+  };
+  const bool ramp = scaling == SAF_ROPE_RAMP;
+  const double lo = ramp ? std::max(std::floor(pair(32.0)), 0.0) : 0.0;
+  const double hi = ramp ? std::min(std::ceil(pair(1.0)), rot_dim - 1.0) : 0.0;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rot_dim);
+    freqs_out[i] = scaling == SAF_ROPE_LINEAR ? f / factor : f;
+    if (ramp) {
+      const double slow = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+      freqs_out[i] = f / factor * slow + f * (1.0 - slow);
+    }
+  }
+  if (mscale_out) *mscale_out = ramp ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return SAF_OK;
+}
+
+namespace {
+
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0; }
+
+// Shapes, dtypes and the strides of the tensors that are there; `cached`: the keys' outputs are the pools (checked by the caller).
+int validate_rotary(const saf_rotary* r, bool cached) {
+  if (!r || r->B < 1 || r->T < 1 || r->Hq < 0 || r->Hk < 0 || r->D < 1 || r->rot_dim < 0 || r->rot_dim > r->D || r->rot_dim % 2 != 0)
+    return SAF_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(r->B) * r->T > 0x7fffffff || r->Hq > 65535 || r->Hk > 65535) return SAF_ERR_INVALID_ARG;
+  if (r->D % 8 != 0 || r->D > 512) return SAF_ERR_UNSUPPORTED;
+  for (int32_t d : {r->in_dtype, r->out_dtype})
+    if (d != SAF_BF16 && d != SAF_F32) return SAF_ERR_UNSUPPORTED;
+  for (int i = cached ? 1 : 0; i < 3; ++i) {
+    if (r->Hq > 0 && (!stride_ok(r->q_strides[i]) || !stride_ok(r->qo_strides[i]))) return SAF_ERR_INVALID_ARG;
+    if (r->Hk > 0 && (!stride_ok(r->k_strides[i]) || (!cached && !stride_ok(r->ko_strides[i])))) return SAF_ERR_INVALID_ARG;
+  }
+  return SAF_OK;
+}
+
+void fill_rotary(RotaryParams* f, const saf_rotary* r) {
+  *f = RotaryParams{};
+  f->tokens = r->B * r->T;
+  f->T = r->T;
+  f->Hq = r->Hq; f->Hk = r->Hk;
+  f->D = r->D; f->rot_dim = r->rot_dim; f->interleaved = r->interleaved ? 1 : 0;
+  f->mscale = r->mscale;
+  for (int i = 0; i < 3; ++i) {
+    f->q_strides[i] = r->q_strides[i];
+    f->k_strides[i] = r->k_strides[i];
+    f->qo_strides[i] = r->qo_strides[i];
+    f->ko_strides[i] = r->ko_strides[i];
+  }
+}
+
+int rotary(saf_ctx* ctx, const saf_rotary* r, const void* q, const void* k, const int32_t* positions, const double* freqs, void* q_out,
+           void* k_out, int backward, void* stream) {
+  if (!ctx) return SAF_ERR_INVALID_ARG;
+  const int rc = validate_rotary(r, false);
+  if (rc) return rc;
+  if (r->Hq + r->Hk == 0) return SAF_OK;
+  if ((r->Hq > 0 && (!q || !q_out || !aligned16(q) || !aligned16(q_out))) ||
+      (r->Hk > 0 && (!k || !k_out || !aligned16(k) || !aligned16(k_out))) || (r->rot_dim > 0 && !freqs))
+    return SAF_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SAF_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ctx->last_stream = st;
+  RotaryParams f;
+  fill_rotary(&f, r);
+  f.backward = backward;
+  f.q = q; f.k = k; f.q_out = q_out; f.k_out = k_out;
+  f.positions = positions;
+  f.freqs = freqs;
+  ScopedTimer timer(ctx, SAF_KERNEL_ROTARY, st);
+  return launch_rotary(f, r->in_dtype == SAF_F32, r->out_dtype == SAF_F32, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+}
+
+int validate_cache(const saf_cache* c) {
+  if (!c || c->R < 1 || c->R > 4096 || c->N < 1 || c->page_size < 1 || c->n_pages < 1 || c->max_pages < 1) return SAF_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(c->page_size) * c->n_pages > 0x7fffffff || static_cast<int64_t>(c->R) * c->max_pages > 0x7fffffff ||
+      static_cast<int64_t>(c->page_size) * c->max_pages > 0x7fffffff)
+    return SAF_ERR_INVALID_ARG;
+  return SAF_OK;
+}
+
+int validate_pools(const saf_cache* c) {
+  if (c->H < 1 || c->kv_group < 0 || (c->kv_group > 1 && c->H % c->kv_group != 0)) return SAF_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (!stride_ok(c->k_strides[i]) || !stride_ok(c->v_strides[i])) return SAF_ERR_INVALID_ARG;
+  return SAF_OK;
+}
+
+}  // namespace
+
+int saf_rotary_fwd(saf_ctx* ctx, const saf_rotary* r, const void* q, const void* k, const int32_t* positions, const double* freqs,
+                   void* q_out, void* k_out, void* stream) {
+  return rotary(ctx, r, q, k, positions, freqs, q_out, k_out, 0, stream);
+}
+
+int saf_rotary_bwd(saf_ctx* ctx, const saf_rotary* r, const void* dq_out, const void* dk_out, const int32_t* positions,
+                   const double* freqs, void* dq, void* dk, void* stream) {
+  return rotary(ctx, r, dq_out, dk_out, positions, freqs, dq, dk, 1, stream);
+}
+
+int saf_cache_plan(saf_ctx* ctx, const saf_cache* c, const int32_t* ctx_lens, const int32_t* new_lens, const int32_t* parents,
+                   const int32_t* held_in, int32_t* held_out, const int32_t* free_count_in, int32_t* free_count_out,
+                   int32_t* free_list, int32_t* block_table, int32_t* new_offsets, int32_t* kv_lens, int32_t* slots,
+                   int32_t* positions, uint64_t* tree_masks, int32_t* missing, void* stream) {
+  if (!ctx) return SAF_ERR_INVALID_ARG;
+  int rc = validate_cache(c);
+  if (rc) return rc;
+  if (!ctx_lens || !new_lens || !held_in || !held_out || !free_count_in || !free_count_out || !free_list || !block_table ||
+      !new_offsets || !kv_lens || !slots || !positions || !missing || (parents == nullptr) != (tree_masks == nullptr))
+    return SAF_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SAF_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ctx->last_stream = st;
+  CachePlanParams f{c->R, c->N, c->page_size, c->n_pages, c->max_pages, ctx_lens, new_lens, parents, held_in, held_out, free_count_in,
+                    free_count_out, free_list, block_table, new_offsets, kv_lens, slots, positions,
+                    reinterpret_cast<unsigned long long*>(tree_masks), missing, ctx->queue_dev + 4};
+  ScopedTimer timer(ctx, SAF_KERNEL_CACHE_PLAN, st);
+  return launch_cache_plan(f, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+}
+
+int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, const void* q, const void* k, const void* v,
+                     const int32_t* slots, const int32_t* positions, const double* freqs, void* q_out, void* k_cache,
+                     void* v_cache, void* stream) {
+  if (!ctx) return SAF_ERR_INVALID_ARG;
+  int rc = validate_cache(c);
+  if (rc || (rc = validate_pools(c)) || (rc = validate_rotary(r, true))) return rc;
+  const int kvg = c->kv_group > 1 ? c->kv_group : 1;
+  if (r->B != 1 || r->T != c->N || r->Hk != c->H / kvg || r->D != c->D) return SAF_ERR_INVALID_ARG;
+  if (r->in_dtype != SAF_BF16 || r->out_dtype != SAF_BF16) return SAF_ERR_UNSUPPORTED;
+  if (!k || !v || !slots || !k_cache || !v_cache || (r->Hq > 0 && (!q || !q_out)) || (r->rot_dim > 0 && (!positions || !freqs)))
+    return SAF_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || (r->Hq > 0 && (!aligned16(q) || !aligned16(q_out))) ||
+      !stride_ok(c->vn_strides[0]) || !stride_ok(c->vn_strides[1]))
+    return SAF_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SAF_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ctx->last_stream = st;
+  RotaryParams f;
+  fill_rotary(&f, r);
+  f.Hv = r->Hk;
+  f.q = q; f.k = k; f.v = v; f.q_out = q_out; f.k_out = k_cache; f.v_out = v_cache;
+  for (int i = 0; i < 3; ++i) {
+    f.ko_strides[i] = c->k_strides[i];
+    f.vo_strides[i] = c->v_strides[i];
+  }
+  f.vn_strides[0] = c->vn_strides[0];
+  f.vn_strides[1] = c->vn_strides[1];
+  f.positions = positions;
+  f.freqs = freqs;
+  f.slots = slots;
+  f.n_slots = c->n_pages * c->page_size;
+  f.page_size = c->page_size;
+  ScopedTimer timer(ctx, SAF_KERNEL_CACHE_APPEND, st);
+  return launch_rotary(f, false, false, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+}
+
+int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* k_cache, const void* v_cache,
+                   const int32_t* block_table, const int32_t* new_offsets, const int32_t* kv_lens, const int32_t* positions,
+                   const uint64_t* tree_masks, const uint8_t* frozen_mask_host, const float* alpha, const float* rho, void* O,
+                   float* LSE, void* stream) {
+  if (!ctx) return SAF_ERR_INVALID_ARG;
+  int rc = validate_cache(c);
+  if (rc || (rc = validate_pools(c))) return rc;
+  if ((c->D != 64 && c->D != 96 && c->D != 128) || c->page_size % 16 != 0 || c->H > CACHE_MAX_HEADS ||
+      (c->o_dtype != SAF_F32 && c->o_dtype != SAF_BF16))
+    return SAF_ERR_UNSUPPORTED;
+  if (!frozen_mask_host || c->max_new < 1 || c->max_new > 64 || c->max_len < 1 ||
+      c->max_len > static_cast<int64_t>(c->max_pages) * c->page_size)
+    return SAF_ERR_INVALID_ARG;
+  CacheAttnParams f{};
+  int nf = 0;
+  for (int h = 0; h < c->H; ++h)
+    if (frozen_mask_host[h]) {
+      f.frozen[h >> 5] |= 1u << (h & 31);
+      ++nf;
+    }
+  const bool ordinary = nf < c->H;
+  if (!v_cache || !O || !block_table || !new_offsets || !kv_lens || (ordinary && (!Q || !k_cache)) || (nf > 0 && (!alpha || !rho || c->Tp < c->max_len)))
+    return SAF_ERR_INVALID_ARG;
+  if (!aligned16(v_cache) || !aligned16(O) || (ordinary && (!aligned16(Q) || !aligned16(k_cache)))) return SAF_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i)
+    if (!stride_ok(c->o_strides[i]) || (ordinary && !stride_ok(c->q_strides[i]))) return SAF_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return SAF_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ctx->last_stream = st;
+  f.R = c->R; f.N = c->N; f.H = c->H; f.D = c->D; f.Tp = c->Tp;
+  f.kv_group = c->kv_group > 1 ? c->kv_group : 1;
+  f.page_size = c->page_size; f.n_pages = c->n_pages; f.max_pages = c->max_pages;
+  f.max_len = c->max_len; f.max_new = c->max_new;
+  f.scale_log2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * 1.4426950408889634f;
+  f.q = Q; f.k = k_cache; f.v = v_cache;
+  for (int i = 0; i < 2; ++i) {
+    f.q_strides[i] = c->q_strides[i];
+    f.o_strides[i] = c->o_strides[i];
+  }
+  for (int i = 0; i < 3; ++i) {
+    f.k_strides[i] = c->k_strides[i];
+    f.v_strides[i] = c->v_strides[i];
+  }
+  f.block_table = block_table; f.new_offsets = new_offsets; f.kv_lens = kv_lens; f.positions = positions;
+  f.masks = reinterpret_cast<const unsigned long long*>(tree_masks);
+  f.alpha = alpha; f.rho = rho;
+  f.O = O; f.o_f32 = c->o_dtype == SAF_F32 ? 1 : 0;
+  f.LSE = LSE;
+  ScopedTimer timer(ctx, SAF_KERNEL_CACHE_ATTN, st);
+  return launch_cache_attn(f, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+}
+
 int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out) {
   if (!ctx) return SAF_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);

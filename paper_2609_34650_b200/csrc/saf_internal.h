@@ -270,6 +270,56 @@ cudaError_t launch_calib_zero(double* a, double* b, int n, cudaStream_t st);
 cudaError_t launch_calib_finalize(float* mean, const double* sumsq, const double* sum_plogp, double* tmp, int H, int T,
                                   double n_total, double* s_var, double* s_kl, int num_sms, cudaStream_t st);
 
+// rotary positions, and a step's new tokens into a paged cache (saf_rotary.cu)
+struct RotaryParams {
+  int tokens, T;                    // tokens = B * T
+  int Hq, Hk, Hv;                   // Hv: new values to be copied (cached step only)
+  int D, rot_dim, interleaved, backward;
+  float mscale;
+  const void* q; const void* k; const void* v;
+  void* q_out; void* k_out; void* v_out;
+  int64_t q_strides[3], k_strides[3], qo_strides[3];   // elements: batch, head, token
+  int64_t ko_strides[3], vo_strides[3];                // cached step: page, head, slot
+  int64_t vn_strides[2];                               // row, head
+  const int* positions;             // [tokens], or NULL: token number modulo T
+  const double* freqs;
+  const int* slots;                 // [tokens]: cached step; rows whose slot is not in [0, n_slots) are skipped
+  int n_slots, page_size;
+  int block_tokens;                 // set by the launcher
+};
+cudaError_t launch_rotary(RotaryParams& p, bool in_f32, bool out_f32, int num_sms, cudaStream_t st);
+
+// plan of a cached step (saf_cache.cu); fields as the arguments of saf_cache_plan
+struct CachePlanParams {
+  int R, N, page_size, n_pages, max_pages;
+  const int* ctx_lens; const int* new_lens; const int* parents;
+  const int* held_in; int* held_out;
+  const int* free_count_in; int* free_count_out;
+  int* free_list; int* block_table;
+  int* new_offsets; int* kv_lens; int* slots; int* positions;
+  unsigned long long* tree_masks;
+  int* missing;
+  int* arrived;                     // counter, zero between launches
+};
+cudaError_t launch_cache_plan(const CachePlanParams& p, int num_sms, cudaStream_t st);
+
+// attention over a paged cache (saf_cache_attn.cu)
+constexpr int CACHE_MAX_HEADS = 1024;
+struct CacheAttnParams {
+  int R, N, H, kv_group, D, Tp;
+  int page_size, n_pages, max_pages, max_len, max_new;
+  float scale_log2;
+  const void* q; const void* k; const void* v;
+  int64_t q_strides[2], o_strides[2], k_strides[3], v_strides[3];
+  const int* block_table; const int* new_offsets; const int* kv_lens; const int* positions;
+  const unsigned long long* masks;
+  const float* alpha; const float* rho;
+  void* O; int o_f32;
+  float* LSE;
+  uint32_t frozen[CACHE_MAX_HEADS / 32];
+};
+cudaError_t launch_cache_attn(const CacheAttnParams& p, int num_sms, cudaStream_t st);
+
 }  // namespace saf
 
 // Trace builds only: per-CTA first/last time stamps (globaltimer, ns) of a kernel, read back by
