@@ -91,7 +91,7 @@ struct saf_ctx {
   int fit_heads = 0;                       // of the last fit, and its per-head hand-over steps (nullptr: direct sums throughout)
   const int* fit_resume = nullptr;
   bool selftest_drop_load = false;         // SAF_SELFTEST_DROP_LOAD=1: see FwdParams::selftest_drop_load
-  DevBuf pat_consts, pat_ok, pat_avec, pat_wvec, pat_bandf, pat_bandb, pat_heads, pat_snap, pat_marks, vt_buf, dot_buf, pg_hlist, pg_delta, pg_items, pg_offsets, fit_buf, calib_tmp;
+  DevBuf pat_consts, pat_ok, pat_avec, pat_wvec, pat_bandf, pat_bandb, pat_heads, pat_snap, pat_marks, vt_buf, dot_buf, pg_hlist, pg_delta, pg_items, pg_offsets, fit_buf, calib_tmp, cattn_buf, cattn_counters;
   std::vector<int> pg_hlist_host, pg_offsets_host;   // host copies of the pattern-gradient tables (upload sources)
   std::vector<PgItem> pg_items_host;
   std::array<int, 5> pg_key = {0, 0, 0, 0, 0};      // (B, frozen heads, T, D, grid) the work list was built for
@@ -627,7 +627,7 @@ int saf_destroy(saf_ctx* ctx) {
     cudaFree(e.offsets_dev);
   }
   DevBuf* pbufs[] = {&ctx->pat_consts, &ctx->pat_ok, &ctx->pat_avec, &ctx->pat_wvec, &ctx->pat_bandf, &ctx->pat_bandb,
-                     &ctx->pat_heads, &ctx->pat_snap, &ctx->pat_marks, &ctx->vt_buf, &ctx->dot_buf, &ctx->pg_hlist, &ctx->pg_delta, &ctx->pg_items, &ctx->pg_offsets, &ctx->fit_buf, &ctx->calib_tmp};
+                     &ctx->pat_heads, &ctx->pat_snap, &ctx->pat_marks, &ctx->vt_buf, &ctx->dot_buf, &ctx->pg_hlist, &ctx->pg_delta, &ctx->pg_items, &ctx->pg_offsets, &ctx->fit_buf, &ctx->calib_tmp, &ctx->cattn_buf, &ctx->cattn_counters};
   for (DevBuf* b : pbufs) release(*b);
   DevBuf* bufs[] = {&ctx->mask_buf, &ctx->logz_buf, &ctx->delta_buf, &ctx->dqacc_buf, &ctx->dkacc_buf, &ctx->dvacc_buf, &ctx->qslot_buf, &ctx->hq, &ctx->hk, &ctx->hv,
                     &ctx->hdo, &ctx->ho, &ctx->hlse, &ctx->hdq, &ctx->hdk, &ctx->hdv, &ctx->halpha, &ctx->hrho,
@@ -1586,6 +1586,19 @@ int validate_cache(const saf_cache* c) {
   return SAF_OK;
 }
 
+// a pool as [pages][heads][slots][features]; box = 64 features x 16 slots, 128-byte swizzle, features beyond D read as zero
+int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides) {
+  const int kvg = c->kv_group > 1 ? c->kv_group : 1;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(c->D), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->H / kvg),
+                        static_cast<cuuint64_t>(c->n_pages)};
+  cuuint64_t gs[3] = {static_cast<cuuint64_t>(strides[2]) * 2, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
+  cuuint32_t box[4] = {64, 16, 1, 1}, es[4] = {1, 1, 1, 1};
+  return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? SAF_OK
+             : SAF_ERR_CUDA;
+}
+
 int validate_pools(const saf_cache* c) {
   if (c->H < 1 || c->kv_group < 0 || (c->kv_group > 1 && c->H % c->kv_group != 0)) return SAF_ERR_INVALID_ARG;
   for (int i = 0; i < 3; ++i)
@@ -1698,22 +1711,35 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.page_size = c->page_size; f.n_pages = c->n_pages; f.max_pages = c->max_pages;
   f.max_len = c->max_len; f.max_new = c->max_new;
   f.scale_log2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * 1.4426950408889634f;
-  f.q = Q; f.k = k_cache; f.v = v_cache;
+  f.q = Q;
   for (int i = 0; i < 2; ++i) {
     f.q_strides[i] = c->q_strides[i];
     f.o_strides[i] = c->o_strides[i];
   }
-  for (int i = 0; i < 3; ++i) {
-    f.k_strides[i] = c->k_strides[i];
-    f.v_strides[i] = c->v_strides[i];
+  for (int hk = 0; hk < c->H / f.kv_group; ++hk) {
+    bool keys = false;
+    for (int h = hk * f.kv_group; h < (hk + 1) * f.kv_group; ++h) keys |= !frozen_mask_host[h];
+    if (keys) f.with_keys[hk >> 5] |= 1u << (hk & 31);
+    f.head_weights += keys ? 2 : 1;
   }
+  f.max_rows = cache_attn_rows(c->max_new, f.kv_group);
+  if ((rc = ensure(ctx->cattn_buf, cache_attn_workspace(f.max_rows, c->D, ctx->num_sms))) ||
+      (rc = ensure(ctx->cattn_counters, ctx->num_sms * sizeof(int))) || (rc = zero_if_fresh(ctx->cattn_counters, st)))
+    return rc;
+  f.workspace = static_cast<float*>(ctx->cattn_buf.ptr);
+  f.counters = static_cast<int*>(ctx->cattn_counters.ptr);
+  f.status = ctx->status_dev;
+  f.wait_limit_ns = ctx->wait_limit_ns;
+  CUtensorMap mk, mv;
+  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides)) || (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides)))
+    return rc;
   f.block_table = block_table; f.new_offsets = new_offsets; f.kv_lens = kv_lens; f.positions = positions;
   f.masks = reinterpret_cast<const unsigned long long*>(tree_masks);
   f.alpha = alpha; f.rho = rho;
   f.O = O; f.o_f32 = c->o_dtype == SAF_F32 ? 1 : 0;
   f.LSE = LSE;
   ScopedTimer timer(ctx, SAF_KERNEL_CACHE_ATTN, st);
-  return launch_cache_attn(f, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+  return launch_cache_attn(mk, mv, f, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
 }
 
 int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out) {
@@ -1726,6 +1752,7 @@ int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out) {
   if (detail_out) *detail_out = word;
   if (word != 0) {
     cudaMemset(ctx->status_dev, 0, sizeof(int));
+    ctx->cattn_counters.fresh = true;        // (blocks that gave up were not counted)
     return SAF_ERR_DEVICE_TIMEOUT;
   }
   return SAF_OK;

@@ -309,16 +309,27 @@ struct CacheAttnParams {
   int R, N, H, kv_group, D, Tp;
   int page_size, n_pages, max_pages, max_len, max_new;
   float scale_log2;
-  const void* q; const void* k; const void* v;
-  int64_t q_strides[2], o_strides[2], k_strides[3], v_strides[3];
+  const void* q;
+  int64_t q_strides[2], o_strides[2];
   const int* block_table; const int* new_offsets; const int* kv_lens; const int* positions;
   const unsigned long long* masks;
   const float* alpha; const float* rho;
   void* O; int o_f32;
   float* LSE;
-  uint32_t frozen[CACHE_MAX_HEADS / 32];
+  int max_rows;                     // rows of a unit's part (cache_attn_rows)
+  int head_weights;                 // sum over the cached heads of what a tile reads (1, or 2 with keys)
+  float* workspace;                 // parts of units that lie in two blocks or more: two of each block
+  int* counters;                    // one a block, zero between launches
+  int stages;                       // set by the launcher
+  int* status;
+  unsigned long long wait_limit_ns;
+  uint32_t frozen[CACHE_MAX_HEADS / 32];     // bit per query head
+  uint32_t with_keys[CACHE_MAX_HEADS / 32];  // bit per cached head: some query head of its group is ordinary
 };
-cudaError_t launch_cache_attn(const CacheAttnParams& p, int num_sms, cudaStream_t st);
+int cache_attn_rows(int max_new, int kv_group);
+size_t cache_attn_workspace(int max_rows, int D, int num_sms);
+// mk, mv: the pools as [pages][heads][slots][features], boxes of 16 slots x 64 features
+cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st);
 
 }  // namespace saf
 
