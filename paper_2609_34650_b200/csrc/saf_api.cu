@@ -1586,13 +1586,13 @@ int validate_cache(const saf_cache* c) {
   return SAF_OK;
 }
 
-// a pool as [pages][heads][slots][features]; box = 64 features x 16 slots, 128-byte swizzle, features beyond D read as zero
-int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides) {
+// a pool as [pages][heads][slots][features]; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D read as zero
+int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, int box_rows) {
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
   cuuint64_t dims[4] = {static_cast<cuuint64_t>(c->D), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->H / kvg),
                         static_cast<cuuint64_t>(c->n_pages)};
   cuuint64_t gs[3] = {static_cast<cuuint64_t>(strides[2]) * 2, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
-  cuuint32_t box[4] = {64, 16, 1, 1}, es[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1}, es[4] = {1, 1, 1, 1};
   return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? SAF_OK
@@ -1731,7 +1731,9 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.status = ctx->status_dev;
   f.wait_limit_ns = ctx->wait_limit_ns;
   CUtensorMap mk, mv;
-  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides)) || (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides)))
+  f.box_rows = cache_attn_box_rows(c->D, c->page_size);
+  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, f.box_rows)) ||
+      (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, f.box_rows)))
     return rc;
   f.block_table = block_table; f.new_offsets = new_offsets; f.kv_lens = kv_lens; f.positions = positions;
   f.masks = reinterpret_cast<const unsigned long long*>(tree_masks);

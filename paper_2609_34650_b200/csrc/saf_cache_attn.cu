@@ -4,13 +4,15 @@
 //   alpha(p_j) + rho(p_i - p_j) (frozen head), running maximum and sum in fp32, in powers of two.
 //
 // Every key and value is read once for all rows that share it, so DRAM bounds the call unless it is a short one.  A unit is one request,
-// one cached head and up to 16 of its rows (new token, query head of the group); its keys come in tiles of 16.  The units' tiles, laid end to end
-// and weighed by what they read (2 for keys and values, 1 where all heads of a group are frozen and only values are read), are cut
-// into equal runs, one for each warp of the grid: no run is longer than another whatever the lengths are, and a single long request fills
-// the GPU like many short ones.  A warp streams its run on its own: it fetches tiles by TMA into a ring of its own, multiplies with
-// 16-row matrix instructions (rows that are not there are zeros: with up to 16 rows a tile costs 32 instructions of 4096 multiply-adds' worth for 8 KB, about
-// a fifth of the tensor cores' time at DRAM speed), and meets other warps only when the run is over, to join what is left of
+// one cached head and up to 8, 16 or 32 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
+// head dimension 64 and 16 above.  The units' tiles, laid end to end and weighed by what they read (2 for keys and values, 1 where all
+// heads of a group are frozen and only values are read), are cut into equal runs, one for each warp of the grid: no run is longer than
+// another whatever the lengths are, and a single long request fills the GPU like many short ones.  A warp streams its run on its
+// own: it fetches tiles by TMA into a ring of its own, and meets other warps only when the run is over, to join what is left of
 // units that were cut: in shared memory within a block, through L2 between blocks, where the block that arrives last joins the parts in order.
+// The products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that keys and features fill the 16-row side of the matrix
+// instructions and the few rows of a step their 8-column side (with rows on the 16-row side the kernel issued twice the
+// instructions, which bound it at 550 a tile of 16 keys).
 #include "ptx.cuh"
 #include "saf_internal.h"
 
@@ -20,16 +22,16 @@
 namespace saf {
 namespace {
 
-constexpr int KT = 16;              // keys of a tile: one step of the second product
-constexpr int ROWS = 16;            // rows of a unit
+constexpr int W = 8;                // warps of a block
+constexpr int TILE = 4096, STAGE = 2 * TILE;   // a tile of keys or values; both
+constexpr int MAX_STAGES = 4;
+constexpr int SINGLE_TILES = 4;     // tiles a warp up to which a block takes a whole unit where there are no more units than blocks
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <int D>
 struct Cfg {
   static constexpr int HALVES = D == 64 ? 1 : 2;              // 64-feature boxes of a tile row (96: zero-filled to 128)
-  static constexpr int TILE = HALVES * KT * 128;              // bytes of a key or value tile
-  static constexpr int STAGE = 2 * TILE;
-  static constexpr int WARPS = D == 64 ? 16 : 8;              // so that a ring of three stages a warp takes 192 KB
+  static constexpr int KT = TILE / (HALVES * 128);            // keys of a tile
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -45,6 +47,13 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// 8 x 8 elements of 16 bits, a pair of a row in each lane, transposed
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
 // Where a run stands: a unit, and its place on the line of all tiles.
 struct Unit {
   long long start;                  // of the unit's first tile on the line
@@ -55,6 +64,7 @@ struct Unit {
 
 __device__ __forceinline__ int weight_of(const CacheAttnParams& p, int hk) { return ((p.with_keys[hk >> 5] >> (hk & 31)) & 1) + 1; }
 
+template <int KT, int ROWS>
 __device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) {
   u.first = min(max(p.new_offsets[u.r], 0), p.N);
   const int last = min(p.new_offsets[u.r + 1], p.N);
@@ -64,6 +74,7 @@ __device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) 
   u.tiles = max((u.len + KT - 1) / KT, 1);                    // (a request without keys still gets its zeros)
 }
 // The next unit that has rows; u.r = p.R behind the last.
+template <int KT, int ROWS>
 __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
   u.start += static_cast<long long>(u.weight) * u.tiles;
   if (++u.rt < u.row_tiles) return;
@@ -72,7 +83,7 @@ __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
     u.hk = 0;
     do {
       if (++u.r >= p.R) return;
-      load_request(p, u);
+      load_request<KT, ROWS>(p, u);
     } while (u.many == 0);
   }
   u.weight = weight_of(p, u.hk);
@@ -81,8 +92,21 @@ __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
 __device__ __forceinline__ int tile_at(const Unit& u, long long x) {
   const long long d = x - u.start;
   if (d <= 0) return 0;
-  return static_cast<int>(min((d + u.weight - 1) / u.weight, static_cast<long long>(u.tiles)));
+  return static_cast<int>(min((d + u.weight - 1) >> (u.weight - 1), static_cast<long long>(u.tiles)));   // (weight 1 or 2)
 }
+// a / b; the 64-bit division takes several hundred clocks
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
+}
+// `total` places in `runs` runs: the first `more` of them have one place more than the others.
+struct Cut {
+  long long total, runs, each, more;
+  __device__ __forceinline__ long long start(long long id) const { return id >= runs ? total : each * id + min(id, more); }
+  __device__ __forceinline__ int run_of(long long x) const {
+    const long long big = more * (each + 1);
+    return static_cast<int>(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
+  }
+};
 
 // A part of a unit's result: rows x D sums, then maxima, then sums of weights; whole 16-byte words, so that parts lie side by side.
 __host__ __device__ constexpr int part_size(int max_rows, int D) { return (max_rows * (D + 2) + 3) / 4 * 4; }
@@ -92,7 +116,7 @@ struct Part {
   int first, many, rt, hk;
 };
 
-template <int D>
+template <int ROWS>
 __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& u, int row, int f, float4 x, float m, float l) {
   const int g = p.kv_group, at = u.rt * ROWS + row, n = u.first + at / g, h = u.hk * g + at % g;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;               // (NaN stays NaN)
@@ -108,20 +132,27 @@ __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& 
   }
 }
 
+// Parts of one unit within a block: order[begin .. begin + count), and the blocks that the unit lies in.
+struct Group {
+  Part unit;
+  int begin, count, c_first, c_last;
+};
+
 // Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.
-template <int D, bool GLOBAL, typename At>
+template <int D, int ROWS, bool GLOBAL, typename At>
 __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, int max_rows, int members, At at, float* dst, int tid, int nthr) {
   const int rows = min(ROWS, u.many * p.kv_group - u.rt * ROWS);
   for (int e = tid; e < rows * (D / 4); e += nthr) {
     const int row = e / (D / 4), f = (e - row * (D / 4)) * 4;
     float m = -INFINITY, l = 0.0f;
+#pragma unroll 8
     for (int i = 0; i < members; ++i) {
       const float* s = at(i) + max_rows * D + row;
       m = fmaxf(m, GLOBAL ? __ldcg(s) : *s);
     }
     const float base = m == -INFINITY ? 0.0f : m;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < members; ++i) {
       const float* s = at(i);
       const float* q = s + max_rows * D + row;
@@ -137,24 +168,29 @@ __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, in
         dst[max_rows * (D + 1) + row] = l;
       }
     } else {
-      write_row<D>(p, u, row, f, x, m, l);
+      write_row<ROWS>(p, u, row, f, x, m, l);
     }
   }
 }
 
-template <int D, bool EXACT>
-__global__ void __launch_bounds__(32 * Cfg<D>::WARPS, 1)
+template <int D, int NB, bool EXACT>
+__global__ void __launch_bounds__(32 * W, 1)
 saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ CacheAttnParams p) {
-  constexpr int W = Cfg<D>::WARPS, TILE = Cfg<D>::TILE, STAGE = Cfg<D>::STAGE, HALVES = Cfg<D>::HALVES, NT = 32 * W;
+  constexpr int HALVES = Cfg<D>::HALVES, KT = Cfg<D>::KT, SUB = KT / 16, NT = 32 * W, ROWS = 8 * NB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int stages = p.stages, max_rows = p.max_rows, part_floats = part_size(max_rows, D);
-  // [warps][stages] tiles, then a part of each warp's run; at the run's end its ring holds a second one
-  float* parts = reinterpret_cast<float*>(smem + W * stages * STAGE);
-  __shared__ uint64_t full[W][4];
+  // [warps][stages] tiles, then a part of each warp's run; at the run's end its ring holds a second one.  Parts of 32 rows, which
+  // would leave no room for the ring, lie in the workspace.
+  auto part_at = [&](int w, int k) -> float* {
+    if (NB > 2) return p.workspace + (static_cast<int64_t>(gridDim.x) * 2 + (static_cast<int64_t>(blockIdx.x) * W + w) * 2 + k) * part_floats;
+    return k == 0 ? reinterpret_cast<float*>(smem + W * stages * STAGE) + w * part_floats : reinterpret_cast<float*>(smem + w * stages * STAGE);
+  };
+  __shared__ uint64_t full[W][MAX_STAGES];
   __shared__ Part meta[W][2];
-  __shared__ long long red[W];
-  __shared__ int abort_s, arrived_s[2];
+  __shared__ long long red[W], red_units[W];
+  __shared__ int red_tiles[W], order[2 * W], open_s[2], counts_s[2], arrived_s[2], abort_s;
+  __shared__ Group groups[2 * W];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) abort_s = 0;
   if (lane < stages) mbar_init(&full[warp][lane], 1);
@@ -171,58 +207,108 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   long long* sums = reinterpret_cast<long long*>(smem);
   const int Hk = p.H / p.kv_group;
   const int per = (p.R + NT - 1) / NT, r0 = min(static_cast<int>(threadIdx.x) * per, p.R), r1 = min(r0 + per, p.R);
-  long long cost = 0;
+  long long cost = 0, units = 0;
+  int longest = 0;
   for (int r = r0; r < r1; ++r) {
     Unit u;
     u.r = r;
-    load_request(p, u);
+    load_request<KT, ROWS>(p, u);
     cost += static_cast<long long>(u.row_tiles) * u.tiles * p.head_weights;
+    units += static_cast<long long>(u.row_tiles) * Hk;
+    if (u.many > 0) longest = max(longest, u.tiles);
     sums[r] = cost;
   }
-  long long scan = cost;
+  long long scan = cost, scan_units = units;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, scan, d);
-    if (lane >= d) scan += y;
+    const long long y = __shfl_up_sync(0xffffffffu, scan, d), z = __shfl_up_sync(0xffffffffu, scan_units, d);
+    if (lane >= d) {
+      scan += y;
+      scan_units += z;
+    }
   }
-  if (lane == 31) red[warp] = scan;
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 31) {
+    red[warp] = scan;
+    red_units[warp] = scan_units;
+    red_tiles[warp] = longest;
+  }
   __syncthreads();
-  long long before = scan - cost, total = 0;
+  long long before = scan - cost, before_units = scan_units - units;
+  Cut cut{0, 0, 0, 0};
+  long long all_units = 0;
   for (int w = 0; w < W; ++w) {
-    const long long s = red[w];
-    if (w < warp) before += s;
-    total += s;
+    const long long s = red[w], n = red_units[w];
+    if (w < warp) {
+      before += s;
+      before_units += n;
+    }
+    cut.total += s;
+    all_units += n;
+    longest = max(longest, red_tiles[w]);
   }
-  for (int r = r0; r < r1; ++r) sums[r] += before;
+  // Few short units: a block each, so that no unit's parts meet through L2.
+  const bool single = all_units <= gridDim.x && longest <= SINGLE_TILES * W;
+  if (single) {
+    if (blockIdx.x >= all_units) return;
+    for (int r = r0; r < r1; ++r) {
+      Unit u;
+      u.r = r;
+      load_request<KT, ROWS>(p, u);
+      sums[r] = before_units += static_cast<long long>(u.row_tiles) * Hk;
+    }
+  } else {
+    for (int r = r0; r < r1; ++r) sums[r] += before;
+  }
   __syncthreads();
-  // runs of at least two whole tiles
-  const long long runs = max(1ll, min(static_cast<long long>(gridDim.x) * W, (total + 3) / 4));
-  auto run_start = [&](long long id) { return total * min(id, runs) / runs; };
-  const long long x0 = run_start(static_cast<long long>(blockIdx.x) * W + warp), x1 = run_start(static_cast<long long>(blockIdx.x) * W + warp + 1);
-  const long long b0 = run_start(static_cast<long long>(blockIdx.x) * W), b1 = run_start(static_cast<long long>(blockIdx.x + 1) * W);
-  if (b0 >= b1) return;
+  long long x0 = blockIdx.x, x1, b0, b1;                     // this warp's run, this block's runs
+  if (!single) {
+    // runs of at least two whole tiles
+    cut.runs = max(1ll, min(static_cast<long long>(gridDim.x) * W, (cut.total + 3) / 4));
+    cut.each = quotient(cut.total, cut.runs);
+    cut.more = cut.total - cut.each * cut.runs;
+    const long long id = static_cast<long long>(blockIdx.x) * W;
+    x0 = cut.start(id + warp);
+    x1 = cut.start(id + warp + 1);
+    b0 = cut.start(id);
+    b1 = cut.start(id + W);
+    if (b0 >= b1) return;
+  }
   Unit u;
   u.r = p.R;
-  if (x0 < x1) {
+  if (single || x0 < x1) {
     int lo = 0, hi = p.R;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (sums[mid] > x0) hi = mid;
       else lo = mid + 1;
     }
-    u.r = lo;                                               // (x0 < total: there is one)
+    u.r = lo;                                               // (x0 is below the total: there is one)
     u.start = lo ? sums[lo - 1] : 0;
-    load_request(p, u);
-    u.hk = 0;
-    u.rt = 0;
-    u.weight = weight_of(p, 0);
-    while (u.start + static_cast<long long>(u.weight) * u.tiles * u.row_tiles <= x0) {
-      u.start += static_cast<long long>(u.weight) * u.tiles * u.row_tiles;
-      u.weight = weight_of(p, ++u.hk);
+    load_request<KT, ROWS>(p, u);
+    if (single) {
+      const int at = static_cast<int>(x0 - u.start);
+      u.hk = at / u.row_tiles;
+      u.rt = at - u.hk * u.row_tiles;
+      u.weight = weight_of(p, u.hk);
+      u.start = 0;
+      b0 = 0;
+      b1 = static_cast<long long>(u.weight) * u.tiles;
+      x0 = u.weight * static_cast<long long>(u.tiles * warp / W);
+      x1 = u.weight * static_cast<long long>(u.tiles * (warp + 1) / W);
+      if (x0 >= x1) u.r = p.R;
+    } else {
+      u.hk = 0;
+      u.rt = 0;
+      u.weight = weight_of(p, 0);
+      while (u.start + static_cast<long long>(u.weight) * u.tiles * u.row_tiles <= x0) {
+        u.start += static_cast<long long>(u.weight) * u.tiles * u.row_tiles;
+        u.weight = weight_of(p, ++u.hk);
+      }
+      const long long skip = quotient(x0 - u.start, static_cast<long long>(u.weight) * u.tiles);
+      u.rt = static_cast<int>(skip);
+      u.start += skip * u.weight * u.tiles;
     }
-    const long long skip = (x0 - u.start) / (static_cast<long long>(u.weight) * u.tiles);
-    u.rt = static_cast<int>(skip);
-    u.start += skip * u.weight * u.tiles;
   }
   __syncthreads();                                          // the sums have been read: the ring may be filled
 
@@ -234,12 +320,12 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   // ---- the fetching end of the run: up to `stages` tiles ahead of the multiplying one
   Unit fu = u;
   int ft = 0, fend = 0, pages_at = 0, page_ids = 0, filled = 0;
-  bool fmore = x0 < x1;
-  auto load_pages = [&](int tile) {                          // lane l: page of tile + l
+  bool fmore = x0 < x1;                                     // (a block of a single unit: warps without a tile have x0 = x1)
+  auto load_pages = [&](int tile) {                          // lane l: page of the 16 keys number tile * SUB + l
     pages_at = tile;
-    const int t = tile + lane;
+    const int c = tile * SUB + lane;
     int id = 0;
-    if (t < fu.tiles && t * KT < p.max_len) id = p.block_table[static_cast<int64_t>(fu.r) * p.max_pages + t * KT / p.page_size];
+    if (c * 16 < max(fu.len, 1)) id = p.block_table[static_cast<int64_t>(fu.r) * p.max_pages + c * 16 / p.page_size];
     page_ids = min(max(id, 0), p.n_pages - 1);
   };
   auto enter = [&]() {                                       // false: the unit has no tile in the run
@@ -249,7 +335,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   };
   auto advance = [&]() {                                     // to the next unit with a tile in the run
     do {
-      next_unit(p, fu);
+      next_unit<KT, ROWS>(p, fu);
       if (fu.r >= p.R || fu.start >= x1) {
         fmore = false;
         return;
@@ -264,18 +350,26 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   auto fetch = [&]() {
     if (!fmore) return;
     const int stage = filled % stages;
-    if (ft - pages_at >= 32) load_pages(ft);
-    const int page = __shfl_sync(0xffffffffu, page_ids, ft - pages_at);
+    if (ft - pages_at >= 32 / SUB) load_pages(ft);
+    int page[SUB];
+#pragma unroll
+    for (int c = 0; c < SUB; ++c) page[c] = __shfl_sync(0xffffffffu, page_ids, (ft - pages_at) * SUB + c);
     const int slot = (ft * KT) % p.page_size;
     const bool keys = fu.weight == 2;
     if (lane == 0) {
       uint8_t* dst = ring + stage * STAGE;
       uint64_t* bar = &full[warp][stage];
-      mbar_expect_tx(bar, keys ? STAGE : TILE);
+      // (32 keys: one box where pages hold whole ones, else two, the second only if there are keys in it)
+      const int boxes = SUB == 2 && p.box_rows == 16 && ft * KT + 16 < fu.len ? 2 : 1;
+      const int bytes = boxes * p.box_rows * 128 * HALVES;
+      mbar_expect_tx(bar, keys ? 2 * bytes : bytes);
+      for (int c = 0; c < boxes; ++c) {
+        const int at = c == 0 ? slot : (ft * KT + 16) % p.page_size, id = c == 0 ? page[0] : page[SUB - 1];
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        if (keys) tma_load_4d(dst + h * KT * 128, &mk, bar, 64 * h, slot, fu.hk, page);
-        tma_load_4d(dst + TILE + h * KT * 128, &mv, bar, 64 * h, slot, fu.hk, page);
+        for (int h = 0; h < HALVES; ++h) {
+          if (keys) tma_load_4d(dst + (h + c) * 2048, &mk, bar, 64 * h, at, fu.hk, id);
+          tma_load_4d(dst + TILE + (h + c) * 2048, &mv, bar, 64 * h, at, fu.hk, id);
+        }
       }
     }
     ++filled;
@@ -289,139 +383,195 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   while (alive && u.r < p.R && u.start < x1) {
     const int t_begin = tile_at(u, x0), t_end = tile_at(u, x1);
     if (t_begin >= t_end) {
-      next_unit(p, u);
+      next_unit<KT, ROWS>(p, u);
       continue;
     }
     const int ctx = u.len - u.many, rows = min(ROWS, u.many * g - u.rt * ROWS);
-    // this thread's two rows
-    int pos[2];
-    bool there[2], frozen[2];
-    unsigned long long mask[2];
-    const float* arow[2];
-    const float* rrow[2];
-    int64_t qoff[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int row = gid + 8 * k;
-      there[k] = row < rows;
-      const int at = there[k] ? u.rt * ROWS + row : u.rt * ROWS;
-      const int i = at / g, h = u.hk * g + at % g, n = u.first + i;
-      frozen[k] = (p.frozen[h >> 5] >> (h & 31)) & 1;
-      mask[k] = p.masks ? p.masks[n] : (2ull << i) - 1;      // (i = 63: all)
-      pos[k] = frozen[k] ? (p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + i, 0)) : 0;
-      arow[k] = p.alpha + static_cast<int64_t>(h) * p.Tp;
-      rrow[k] = p.rho + static_cast<int64_t>(h) * p.Tp;
-      qoff[k] = n * p.q_strides[0] + h * p.q_strides[1];
-      if (!there[k]) frozen[k] = false;
-    }
-    const bool any_frozen = __any_sync(0xffffffffu, frozen[0] || frozen[1]);
     const bool keys = u.weight == 2;
-    uint32_t q[D / 16][4];
+    // queries, as columns: column gid of each block of eight rows
+    uint32_t q[NB][D / 16][2];
     if (keys) {
-      const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(p.q);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+      for (int b = 0; b < NB; ++b) {
+        const int at = u.rt * ROWS + min(8 * b + gid, rows - 1), h = u.hk * g + at % g;
+        const bool use = 8 * b + gid < rows && !((p.frozen[h >> 5] >> (h & 31)) & 1);
+        const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(u.first + at / g) * p.q_strides[0] + h * p.q_strides[1] + t2;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int k = e & 1;
-          q[ks][e] = there[k] && !frozen[k] ? *reinterpret_cast<const uint32_t*>(Q + qoff[k] + ks * 16 + (e >> 1) * 8 + t2) : 0u;
-        }
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) q[b][ks][e] = use ? *reinterpret_cast<const uint32_t*>(Q + ks * 16 + e * 8) : 0u;
+      }
     }
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+    // scores and weights: rows 8 b + t2 + e, keys gid and gid + 8 of each 16
+    int pos[NB][2];
+    bool frozen[NB][2];
+    unsigned long long mask[NB][2];                            // of the new tokens that a row sees; a row that is not there sees nothing
+    const float* arow[NB][2];
+    const float* rrow[NB][2];
+    bool any = false;
 #pragma unroll
-    for (int f = 0; f < D / 8; ++f)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[f][e] = 0.0f;
-
+      for (int e = 0; e < 2; ++e) {
+        const int row = 8 * b + t2 + e, at = u.rt * ROWS + min(row, rows - 1), i = at / g, h = u.hk * g + at % g, n = u.first + i;
+        frozen[b][e] = (p.frozen[h >> 5] >> (h & 31)) & 1;
+        any |= frozen[b][e];
+        mask[b][e] = p.masks ? p.masks[n] : (2ull << i) - 1;   // (i = 63: all)
+        pos[b][e] = frozen[b][e] ? (p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + i, 0)) : 0;
+        arow[b][e] = p.alpha + static_cast<int64_t>(h) * p.Tp;
+        rrow[b][e] = p.rho + static_cast<int64_t>(h) * p.Tp;
+      }
+    const bool any_frozen = __any_sync(0xffffffffu, any);
+    float o[NB][D / 16][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[b][f][e] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[b][e] = -INFINITY;
+        l[b][e] = 0.0f;
+      }
+    }
+    // frozen rows: this thread's preferences of a tile, fetched while the tile before is worked on (index: block, 16 keys, key half, row)
+    constexpr int NP = NB * SUB * 4;
+    float fa[NB > 2 ? 1 : NP], fr[NB > 2 ? 1 : NP];
+    auto preference = [&](int t, int x, float& a, float& r) {
+      const int b = x / (SUB * 4), sub = x / 4 % SUB, e = x & 1;
+      const int j = t * KT + sub * 16 + ((x >> 1) & 1) * 8 + gid, back = j - ctx;
+      a = -INFINITY;
+      r = 0.0f;
+      if (frozen[b][e] && j < u.len) {
+        const int pj = back < 0 || !p.positions ? j : min(max(p.positions[u.first + back], 0), p.Tp - 1);
+        if (pj <= pos[b][e]) {
+          a = arow[b][e][pj];
+          r = rrow[b][e][pos[b][e] - pj];
+        }
+      }
+    };
+    auto prefer = [&](int t) {
+      if constexpr (NB <= 2) {
+#pragma unroll
+        for (int x = 0; x < NP; ++x) preference(t, x, fa[x], fr[x]);
+      }
+    };
+    if (any_frozen) prefer(t_begin);
     for (int t = t_begin; t < t_end; ++t) {
       const int stage = used % stages;
       const uint32_t ks_addr = ring_s + stage * STAGE, vs_addr = ks_addr + TILE;
       const int j0 = t * KT;
       const bool tail = j0 + KT > ctx;
-      // frozen rows: this thread's preferences, fetched while the tile is waited for
-      float fs[2][4];
-      if (any_frozen) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = j0 + (e >> 1) * 8 + t2 + (e & 1), back = j - ctx;
-            fs[k][e] = -INFINITY;
-            if (frozen[k] && j < u.len) {
-              const int pj = back < 0 || !p.positions ? j : min(max(p.positions[u.first + back], 0), p.Tp - 1);
-              if (pj <= pos[k]) fs[k][e] = (arow[k][pj] + rrow[k][pos[k] - pj]) * LOG2E;
-            }
-          }
-      }
       if (!mbar_wait_warp_compact(&full[warp][stage], (used / stages) & 1, wc, 90)) {
         alive = false;
         break;
       }
-      float s[2][4];
+      // s[b][sub][2 half + e]: key 16 sub + 8 half + gid, row 8 b + t2 + e
+      float s[NB][SUB][4];
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[k][e] = 0.0f;
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[b][sub][e] = 0.0f;
       if (keys) {
-        // s[nt][2 k + e]: row gid + 8 k, key 8 nt + t2 + e
+        const int row = (((lane >> 3) & 1) << 3) + (lane & 7);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          uint32_t b[4];
-          const int row = ((lane >> 4) << 3) + (lane & 7), chunk = (ks & 3) * 2 + ((lane >> 3) & 1);
-          ldsm4(ks_addr + (ks >> 2) * (KT * 128) + row * 128 + ((chunk ^ (row & 7)) << 4), b);
-          mma16816(s[0], q[ks], b[0], b[1]);
-          mma16816(s[1], q[ks], b[2], b[3]);
-        }
-      }
-      float top[2] = {m[0], m[1]};
+        for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+          for (int sub = 0; sub < SUB; ++sub) {
+            uint32_t a[4];
+            ldsm4(ks_addr + (ks >> 2) * 2048 + (sub * 16 + row) * 128 + ((((ks & 3) * 2 + (lane >> 4)) ^ (row & 7)) << 4), a);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int k = e >> 1;
-          float x = frozen[k] ? fs[k][nt * 2 + (e & 1)] : s[nt][e] * p.scale_log2;
-          if (tail) {
-            const int j = j0 + nt * 8 + t2 + (e & 1), back = j - ctx;
-            if (j >= u.len || (back >= 0 && !((mask[k] >> back) & 1))) x = -INFINITY;
+            for (int b = 0; b < NB; ++b) mma16816(s[b][sub], a, q[b][ks][0], q[b][ks][1]);
           }
-          if (!there[k]) x = -INFINITY;
-          s[nt][e] = x;
-          top[k] = fmaxf(top[k], x);
-        }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
-        top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][sub][e] *= p.scale_log2;
       }
-      if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+      if (any_frozen) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float c = top[k] == -INFINITY ? 1.0f : ex2_approx(m[k] - top[k]);
-          m[k] = top[k];
-          l[k] *= c;
-#pragma unroll
-          for (int f = 0; f < D / 8; ++f) {
-            o[f][2 * k] *= c;
-            o[f][2 * k + 1] *= c;
+        for (int x = 0; x < NP; ++x) {
+          const int b = x / (SUB * 4), sub = x / 4 % SUB;
+          float a, r;
+          if constexpr (NB <= 2) {
+            a = fa[x];
+            r = fr[x];
+          } else {
+            preference(t, x, a, r);
           }
+          if (frozen[b][x & 1]) s[b][sub][x & 3] = (a + r) * LOG2E;
         }
+        if (t + 1 < t_end) prefer(t + 1);
       }
-      const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+      if (tail) {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int k = e >> 1;
-          s[nt][e] = ex2_approx(s[nt][e] - base[k]);
-          l[k] += s[nt][e];
+          for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = j0 + sub * 16 + (e >> 1) * 8 + gid, back = j - ctx;
+              if (j >= u.len || (back >= 0 && !((mask[b][e & 1] >> back) & 1))) s[b][sub][e] = -INFINITY;
+            }
+      }
+      float top[NB][2];
+      bool grown = false;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = m[b][e];
+#pragma unroll
+          for (int sub = 0; sub < SUB; ++sub) x = max3(x, s[b][sub][e], s[b][sub][2 + e]);
+          top[b][e] = x;
+          grown |= x > m[b][e];
+        }
+      // the maximum is only looked for across the lanes where a lane found a larger one
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = top[b][e];
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float c = x == -INFINITY ? 1.0f : ex2_approx(m[b][e] - x);
+            m[b][e] = x;
+            l[b][e] *= c;
+#pragma unroll
+            for (int f = 0; f < D / 16; ++f) {
+              o[b][f][e] *= c;
+              o[b][f][2 + e] *= c;
+            }
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float base = m[b][e] == -INFINITY ? 0.0f : m[b][e];
+#pragma unroll
+          for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const float x = ex2_approx(s[b][sub][2 * half + e] - base);
+              s[b][sub][2 * half + e] = x;
+              l[b][e] += x;
+            }
         }
       if (tail) {
         // values behind the last key are whatever the page held, and a value that some rows do not see may be NaN or infinite: both
         // are zeroed for the product, the second kind added by hand to the rows that see it
         bool wild = false;
-        for (int c = lane; c < KT * HALVES * 8; c += 32) {
-          const int row = c & (KT - 1), rest = c >> 4;
-          const uint32_t addr = vs_addr + (rest >> 3) * (KT * 128) + row * 128 + (((rest & 7) ^ (row & 7)) << 4);
+        for (int c = lane; c < TILE / 16; c += 32) {
+          const int row = (c >> 3) & (KT - 1);
+          const uint32_t addr = vs_addr + c * 16;             // (the swizzle moves 16-byte words within a row)
           uint32_t w[4];
           asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
           if (j0 + row >= u.len) {
@@ -433,32 +583,31 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         }
         __syncwarp();
         if (__any_sync(0xffffffffu, wild)) {
-          for (int key = 0; key < KT; ++key) {
-            const int src = (lane & ~3) | ((key & 7) >> 1);
-            float w[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float a = (key & 1) ? s[0][2 * k + 1] : s[0][2 * k], b = (key & 1) ? s[1][2 * k + 1] : s[1][2 * k];
-              w[k] = __shfl_sync(0xffffffffu, key < 8 ? a : b, src);
-            }
+          for (int sub = 0; sub < SUB; ++sub)
+            for (int key = 0; key < 16; ++key) {
+              const int src = ((key & 7) << 2) | (lane & 3), row = sub * 16 + key;
+              float w[NB][2];
 #pragma unroll
-            for (int f = 0; f < D / 8; ++f) {
-              const uint32_t addr = vs_addr + (f >> 3) * (KT * 128) + key * 128 + (((f & 7) ^ (key & 7)) << 4) + t2 * 2;
-              uint32_t v;
-              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-              const bool lo = (v & 0x7f80u) == 0x7f80u, hi = (v & 0x7f800000u) == 0x7f800000u;
-              if (lo || hi) {
+              for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  if (w[k] == 0.0f) continue;
-                  if (lo) o[f][2 * k] += w[k] * __uint_as_float(v << 16);
-                  if (hi) o[f][2 * k + 1] += w[k] * __uint_as_float(v & 0xffff0000u);
+                for (int e = 0; e < 2; ++e) w[b][e] = __shfl_sync(0xffffffffu, key < 8 ? s[b][sub][e] : s[b][sub][2 + e], src);
+#pragma unroll
+              for (int f = 0; f < D / 8; ++f) {
+                const uint32_t addr = vs_addr + (f >> 3) * 2048 + row * 128 + (((f & 7) ^ (row & 7)) << 4) + gid * 2;
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+                if ((v & 0x7f80u) == 0x7f80u) {
+#pragma unroll
+                  for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                      if (w[b][e] != 0.0f) o[b][f >> 1][(f & 1) * 2 + e] += w[b][e] * __uint_as_float(static_cast<uint32_t>(v) << 16);
                 }
               }
             }
-          }
           __syncwarp();
-          for (int c = lane; c < KT * HALVES * 32; c += 32) {   // (every word of the tile, wherever the swizzle put it)
+          for (int c = lane; c < TILE / 4; c += 32) {
             const uint32_t addr = vs_addr + c * 4;
             uint32_t v;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
@@ -470,26 +619,31 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         }
       }
       // second product.  EXACT (fp32 output): weights as three bf16 terms, 24 bits; else rounded to bf16 once (the output is, too)
-      uint32_t a[EXACT ? 3 : 1][4];
+      const int key = ((lane >> 4) << 3) + (lane & 7);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {                           // a[e]: row gid + 8 (e & 1), keys 8 (e >> 1) + t2, + 1
-        float lo = s[e >> 1][2 * (e & 1)], hi = s[e >> 1][2 * (e & 1) + 1];
+      for (int sub = 0; sub < SUB; ++sub) {
+        uint32_t w[NB][EXACT ? 3 : 1][2];
 #pragma unroll
-        for (int i = 0; i < (EXACT ? 3 : 1); ++i) {
-          a[i][e] = pack_bf16x2(lo, hi);
-          lo -= __uint_as_float(a[i][e] << 16);
-          hi -= __uint_as_float(a[i][e] & 0xffff0000u);
-        }
-      }
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int fb = 0; fb < D / 16; ++fb) {
-        uint32_t b[4];
-        const int row = (((lane >> 3) & 1) << 3) + (lane & 7), chunk = (fb & 3) * 2 + (lane >> 4);
-        ldsm4t(vs_addr + (fb >> 2) * (KT * 128) + row * 128 + ((chunk ^ (row & 7)) << 4), b);
+          for (int half = 0; half < 2; ++half) {
+            float lo = s[b][sub][2 * half], hi = s[b][sub][2 * half + 1];
 #pragma unroll
-        for (int i = 0; i < (EXACT ? 3 : 1); ++i) {
-          mma16816(o[2 * fb], a[i], b[0], b[1]);
-          mma16816(o[2 * fb + 1], a[i], b[2], b[3]);
+            for (int i = 0; i < (EXACT ? 3 : 1); ++i) {
+              const uint32_t x = pack_bf16x2(lo, hi);
+              lo -= __uint_as_float(x << 16);
+              hi -= __uint_as_float(x & 0xffff0000u);
+              w[b][i][half] = transpose8(x);
+            }
+          }
+#pragma unroll
+        for (int f = 0; f < D / 16; ++f) {
+          uint32_t a[4];
+          ldsm4t(vs_addr + (f >> 2) * 2048 + (sub * 16 + key) * 128 + ((((f & 3) * 2 + ((lane >> 3) & 1)) ^ (key & 7)) << 4), a);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < (EXACT ? 3 : 1); ++i) mma16816(o[b][f], a, w[b][i][0], w[b][i][1]);
         }
       }
       if (tail) fence_proxy_async_smem();                     // (the tile may have been written to: before it is fetched over)
@@ -498,10 +652,11 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       fetch();
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
-      l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
-    }
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
     const Part me{u.start, u.start + static_cast<long long>(u.weight) * (u.tiles - 1), u.first, u.many, u.rt, u.hk};
     if (!alive) {
       // given up: the copies in flight end before the block does (a bounded wait again), nothing is joined
@@ -509,119 +664,146 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         for (int spin = 0; spin < 100000 && !mbar_try_wait(&full[warp][i % stages], (i / stages) & 1); ++spin) {
         }
     } else if (t_begin == 0 && t_end == u.tiles) {
+      // pairs of lanes exchange, the one taking the even row, the other the odd one, two features each
+      const int odd = gid & 1;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        // pairs of lanes put four features together
+      for (int b = 0; b < NB; ++b) {
+        const int row = 8 * b + t2 + odd, at = u.rt * ROWS + row, n = u.first + at / g, h = u.hk * g + at % g;
+        const float ls = l[b][odd], inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+        const int64_t off = static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + (gid & ~1);
 #pragma unroll
         for (int f = 0; f < D / 8; ++f) {
-          const float a = o[f][2 * k], b = o[f][2 * k + 1];
-          const float c = __shfl_xor_sync(0xffffffffu, a, 1), d = __shfl_xor_sync(0xffffffffu, b, 1);
-          if (there[k] && (lane & 1) == 0) write_row<D>(p, me, gid + 8 * k, f * 8 + t2, make_float4(a, b, c, d), m[k], l[k]);
+          const float lo = o[b][f >> 1][(f & 1) * 2], hi = o[b][f >> 1][(f & 1) * 2 + 1];
+          const float got = __shfl_xor_sync(0xffffffffu, odd ? lo : hi, 4);
+          const float x = (odd ? got : lo) * inv, y = (odd ? hi : got) * inv;
+          if (row < rows) {
+            if (p.o_f32) *reinterpret_cast<float2*>(static_cast<float*>(p.O) + off + f * 8) = make_float2(x, y);
+            else *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.O) + off + f * 8) = pack_bf16x2(x, y);
+          }
+        }
+        if (row < rows && gid < 2 && p.LSE) {
+          const bool fz = (p.frozen[h >> 5] >> (h & 31)) & 1;
+          p.LSE[static_cast<int64_t>(n) * p.H + h] = fz ? 0.0f : ls == 0.0f ? -INFINITY : (m[b][odd] + log2f(ls)) * LN2;
         }
       }
     } else {
       // the part of a unit that goes on elsewhere: at most two a run, the second when nothing more is fetched
-      float* dst = n_parts == 0 ? parts + warp * part_floats : reinterpret_cast<float*>(ring);
+      float* dst = part_at(warp, n_parts);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int row = gid + 8 * k;
-        if (there[k]) {
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int f = 0; f < D / 8; ++f) *reinterpret_cast<float2*>(dst + row * D + f * 8 + t2) = make_float2(o[f][2 * k], o[f][2 * k + 1]);
-          if ((lane & 3) == 0) {
-            dst[max_rows * D + row] = m[k];
-            dst[max_rows * (D + 1) + row] = l[k];
+        for (int e = 0; e < 2; ++e) {
+          const int row = 8 * b + t2 + e;
+          if (row < rows) {
+#pragma unroll
+            for (int f = 0; f < D / 8; ++f) dst[row * D + f * 8 + gid] = o[b][f >> 1][(f & 1) * 2 + e];
+            if (gid == 0) {
+              dst[max_rows * D + row] = m[b][e];
+              dst[max_rows * (D + 1) + row] = l[b][e];
+            }
           }
         }
-      }
       if (lane == 0) meta[warp][n_parts] = me;
       ++n_parts;
     }
-    next_unit(p, u);
+    next_unit<KT, ROWS>(p, u);
   }
-  // ---- what is left of cut units, in the order of the runs
+  // ---- what is left of cut units, in the order of the runs: warp 0 finds what belongs together, a lane for each part
   __syncthreads();
-  auto part_of = [&](int i) { return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * stages * STAGE) : parts + (i >> 1) * part_floats; };
-  const Part* flat = &meta[0][0];
-  auto block_of = [&](long long x) { return static_cast<int>(((x + 1) * runs - 1) / total / W); };
-  int group = 0, n_open = 0;
-  int open[2];
-  for (int i = 0; i < 2 * W;) {
-    if (flat[i].start < 0) {
-      ++i;
-      continue;
-    }
-    int members = 1, nexti = i + 1;
-    int idx_last = i;
-    for (; nexti < 2 * W; ++nexti) {
-      if (flat[nexti].start < 0) continue;
-      if (flat[nexti].start != flat[i].start) break;
-      ++members;
-      idx_last = nexti;
-    }
-    const Part unit = flat[i];
-    // (members are the parts in [i, idx_last] that are there)
-    auto member = [&](int k) {
-      int at = i;
-      for (int c = 0;; ++at) {
-        if (flat[at].start < 0) continue;
-        if (c++ == k) break;
+  if (warp == 0) {
+    const Part mine = lane < 2 * W ? (&meta[0][0])[lane] : Part{-1, 0, 0, 0, 0, 0};
+    const uint32_t below = (1u << lane) - 1;
+    const uint32_t there = __ballot_sync(0xffffffffu, mine.start >= 0);
+    const long long prior = __shfl_sync(0xffffffffu, mine.start, (there & below) ? 31 - __clz(there & below) : 0);
+    const bool leads = mine.start >= 0 && (!(there & below) || prior != mine.start);
+    const uint32_t leaders = __ballot_sync(0xffffffffu, leads);
+    const int at = __popc(there & below);
+    if (mine.start >= 0) order[at] = lane;
+    bool open = false;
+    const int me = __popc(leaders & below);
+    if (leads) {
+      const uint32_t later = leaders & ~below & ~(1u << lane);
+      const int end = later ? __popc(there & ((1u << (__ffs(later) - 1)) - 1)) : __popc(there);
+      Group& gr = groups[me];
+      gr.unit = mine;
+      gr.begin = at;
+      gr.count = end - at;
+      gr.c_first = gr.c_last = 0;
+      if (!single && (mine.start < b0 || mine.last >= b1)) {
+        gr.c_first = cut.run_of(mine.start) / W;
+        gr.c_last = cut.run_of(mine.last) / W;
+        open = true;
       }
-      return part_of(at);
-    };
-    (void)idx_last;
-    const int c_first = block_of(unit.start), c_last = block_of(unit.last);
-    if (c_first == c_last) {
-      if (group % W == warp) join<D, false>(p, unit, max_rows, members, member, nullptr, lane, 32);
-      ++group;
-    } else {
-      float* dst = p.workspace + (static_cast<int64_t>(blockIdx.x) * 2 + (b0 >= unit.start ? 0 : 1)) * part_floats;
-      join<D, false>(p, unit, max_rows, members, member, dst, threadIdx.x, NT);
-      if (n_open < 2) open[n_open++] = i;
     }
-    i = nexti;
+    const uint32_t opens = __ballot_sync(0xffffffffu, open);
+    if (open) open_s[__popc(opens & below)] = me;            // (a block's first and last unit at most)
+    if (lane == 0) {
+      counts_s[0] = __popc(leaders);
+      counts_s[1] = __popc(opens);
+    }
+  }
+  __syncthreads();
+  auto part_of = [&](int i) -> const float* { return part_at(i >> 1, i & 1); };
+  const int n_groups = counts_s[0], n_open = counts_s[1];
+  auto slot_of = [&](int block, long long first_place, const Part& unit) {
+    return p.workspace + (static_cast<int64_t>(block) * 2 + (first_place >= unit.start ? 0 : 1)) * part_floats;
+  };
+  for (int k = 0; k < n_open; ++k) {
+    const Group& gr = groups[open_s[k]];
+    join<D, ROWS, false>(p, gr.unit, max_rows, gr.count, [&](int i) { return part_of(order[gr.begin + i]); }, slot_of(blockIdx.x, b0, gr.unit), threadIdx.x, NT);
+  }
+  if (n_open > 0) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < n_open) {
+      const Group& gr = groups[open_s[threadIdx.x]];
+      int* counter = p.counters + gr.c_first;
+      const bool last = atomicAdd(counter, 1) == gr.c_last - gr.c_first;
+      arrived_s[threadIdx.x] = last;
+      if (last) *counter = 0;
+      __threadfence();
+    }
+  }
+  for (int k = 0, turn = 0; k < n_groups; ++k) {
+    const Group& gr = groups[k];
+    if (gr.c_first != gr.c_last) continue;
+    if (turn++ % W == warp) join<D, ROWS, false>(p, gr.unit, max_rows, gr.count, [&](int i) { return part_of(order[gr.begin + i]); }, nullptr, lane, 32);
   }
   if (n_open == 0) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x < n_open) {
-    const Part& unit = flat[open[threadIdx.x]];
-    const int c_first = block_of(unit.start), c_last = block_of(unit.last);
-    int* counter = p.counters + c_first;
-    const int before_me = atomicAdd(counter, 1);
-    arrived_s[threadIdx.x] = before_me == c_last - c_first;
-    if (before_me == c_last - c_first) *counter = 0;
-    __threadfence();
-  }
   __syncthreads();
   for (int k = 0; k < n_open; ++k) {
     if (!arrived_s[k]) continue;
-    const Part unit = flat[open[k]];
-    const int c_first = block_of(unit.start), c_last = block_of(unit.last);
-    auto member = [&](int i) {
-      const int c = c_first + i;
-      return p.workspace + (static_cast<int64_t>(c) * 2 + (run_start(static_cast<long long>(c) * W) >= unit.start ? 0 : 1)) * part_floats;
-    };
-    join<D, true>(p, unit, max_rows, c_last - c_first + 1, member, nullptr, threadIdx.x, NT);
+    const Group& gr = groups[open_s[k]];
+    join<D, ROWS, true>(p, gr.unit, max_rows, gr.c_last - gr.c_first + 1,
+                  [&](int i) { return slot_of(gr.c_first + i, cut.start(static_cast<long long>(gr.c_first + i) * W), gr.unit); }, nullptr, threadIdx.x, NT);
   }
 }
 
-template <int D>
+template <int D, int NB>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
-  constexpr int W = Cfg<D>::WARPS;
-  const size_t parts = static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
-  p.stages = static_cast<int>(std::min<size_t>(4, (224 * 1024 - parts) / (static_cast<size_t>(W) * Cfg<D>::STAGE)));
-  const size_t smem = static_cast<size_t>(W) * p.stages * Cfg<D>::STAGE + parts + 1024;
-  auto kernel = p.o_f32 ? saf_cache_attn_kernel<D, true> : saf_cache_attn_kernel<D, false>;
+  const size_t parts = NB > 2 ? 0 : static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
+  p.stages = static_cast<int>(std::min<size_t>(MAX_STAGES, (222 * 1024 - parts) / (W * STAGE)));
+  const size_t smem = static_cast<size_t>(W) * p.stages * STAGE + parts + 1024;
+  auto kernel = p.o_f32 ? saf_cache_attn_kernel<D, NB, true> : saf_cache_attn_kernel<D, NB, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   return launch_pdl(PDL_REST, kernel, num_sms, 32 * W, smem, st, mk, mv, p);
 }
+template <int D>
+cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
+  if (p.max_rows <= 8) return launch<D, 1>(mk, mv, p, num_sms, st);
+  if (p.max_rows <= 16) return launch<D, 2>(mk, mv, p, num_sms, st);
+  return launch<D, 4>(mk, mv, p, num_sms, st);
+}
 
 }  // namespace
 
-int cache_attn_rows(int max_new, int kv_group) { return std::min(ROWS, max_new * kv_group); }
-size_t cache_attn_workspace(int max_rows, int D, int num_sms) { return static_cast<size_t>(num_sms) * 2 * part_size(max_rows, D) * sizeof(float); }
+int cache_attn_rows(int max_new, int kv_group) { return std::min(32, max_new * kv_group); }
+// two parts of each block, and with 32-row units two of each warp
+size_t cache_attn_workspace(int max_rows, int D, int num_sms) {
+  return static_cast<size_t>(num_sms) * (max_rows > 16 ? 2 + 2 * W : 2) * part_size(max_rows, D) * sizeof(float);
+}
+int cache_attn_box_rows(int D, int page_size) { return D == 64 && page_size % 32 == 0 ? 32 : 16; }
 
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
   if (p.D == 64) return launch<64>(mk, mv, p, num_sms, st);

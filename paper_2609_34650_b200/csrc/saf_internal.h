@@ -320,6 +320,7 @@ struct CacheAttnParams {
   int head_weights;                 // sum over the cached heads of what a tile reads (1, or 2 with keys)
   float* workspace;                 // parts of units that lie in two blocks or more: two of each block
   int* counters;                    // one a block, zero between launches
+  int box_rows;                     // slots of a TMA box (cache_attn_box_rows)
   int stages;                       // set by the launcher
   int* status;
   unsigned long long wait_limit_ns;
@@ -328,7 +329,8 @@ struct CacheAttnParams {
 };
 int cache_attn_rows(int max_new, int kv_group);
 size_t cache_attn_workspace(int max_rows, int D, int num_sms);
-// mk, mv: the pools as [pages][heads][slots][features], boxes of 16 slots x 64 features
+int cache_attn_box_rows(int D, int page_size);
+// mk, mv: the pools as [pages][heads][slots][features], boxes of p.box_rows slots x 64 features
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st);
 
 }  // namespace saf
