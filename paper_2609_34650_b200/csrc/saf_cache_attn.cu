@@ -4,7 +4,7 @@
 //   alpha(p_j) + rho(p_i - p_j) (frozen head), running maximum and sum in fp32, in powers of two.
 //
 // Every key and value is read once for all rows that share it, so DRAM bounds the call unless it is a short one.  A unit is one request,
-// one cached head and up to 8, 16 or 32 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
+// one cached head and up to 8 or 16 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
 // head dimension 64 and 16 above.  The units' tiles, laid end to end and weighed by what they read (2 for keys and values, 1 where all
 // heads of a group are frozen and only values are read), are cut into equal runs, one for each warp of the grid: no run is longer than
 // another whatever the lengths are, and a single long request fills the GPU like many short ones.  A warp streams its run on its
@@ -180,10 +180,8 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int stages = p.stages, max_rows = p.max_rows, part_floats = part_size(max_rows, D);
-  // [warps][stages] tiles, then a part of each warp's run; at the run's end its ring holds a second one.  Parts of 32 rows, which
-  // would leave no room for the ring, lie in the workspace.
+  // [warps][stages] tiles, then a part of each warp's run; at the run's end its ring holds a second one
   auto part_at = [&](int w, int k) -> float* {
-    if (NB > 2) return p.workspace + (static_cast<int64_t>(gridDim.x) * 2 + (static_cast<int64_t>(blockIdx.x) * W + w) * 2 + k) * part_floats;
     return k == 0 ? reinterpret_cast<float*>(smem + W * stages * STAGE) + w * part_floats : reinterpret_cast<float*>(smem + w * stages * STAGE);
   };
   __shared__ uint64_t full[W][MAX_STAGES];
@@ -409,6 +407,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     const float* arow[NB][2];
     const float* rrow[NB][2];
     bool any = false;
+    int lead = ROWS;                                          // first frozen row seen
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -416,12 +415,28 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         const int row = 8 * b + t2 + e, at = u.rt * ROWS + min(row, rows - 1), i = at / g, h = u.hk * g + at % g, n = u.first + i;
         frozen[b][e] = (p.frozen[h >> 5] >> (h & 31)) & 1;
         any |= frozen[b][e];
+        if (frozen[b][e]) lead = min(lead, min(row, rows - 1));
         mask[b][e] = p.masks ? p.masks[n] : (2ull << i) - 1;   // (i = 63: all)
         pos[b][e] = frozen[b][e] ? (p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + i, 0)) : 0;
         arow[b][e] = p.alpha + static_cast<int64_t>(h) * p.Tp;
         rrow[b][e] = p.rho + static_cast<int64_t>(h) * p.Tp;
       }
     const bool any_frozen = __any_sync(0xffffffffu, any);
+    if (any_frozen) {
+      // rows of ordinary heads look where the unit's first frozen row looks, so that their loads cost nothing
+      const int first_row = __reduce_min_sync(0xffffffffu, lead);
+      const int at = u.rt * ROWS + first_row, h = u.hk * g + at % g, n = u.first + at / g;
+      const int ps = p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + at / g, 0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (!frozen[b][e]) {
+            arow[b][e] = p.alpha + static_cast<int64_t>(h) * p.Tp;
+            rrow[b][e] = p.rho + static_cast<int64_t>(h) * p.Tp;
+            pos[b][e] = ps;
+          }
+    }
     float o[NB][D / 16][4], m[NB][2], l[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -437,24 +452,30 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     }
     // frozen rows: this thread's preferences of a tile, fetched while the tile before is worked on (index: block, 16 keys, key half, row)
     constexpr int NP = NB * SUB * 4;
-    float fa[NB > 2 ? 1 : NP], fr[NB > 2 ? 1 : NP];
-    auto preference = [&](int t, int x, float& a, float& r) {
-      const int b = x / (SUB * 4), sub = x / 4 % SUB, e = x & 1;
-      const int j = t * KT + sub * 16 + ((x >> 1) & 1) * 8 + gid, back = j - ctx;
-      a = -INFINITY;
-      r = 0.0f;
-      if (frozen[b][e] && j < u.len) {
-        const int pj = back < 0 || !p.positions ? j : min(max(p.positions[u.first + back], 0), p.Tp - 1);
-        if (pj <= pos[b][e]) {
-          a = arow[b][e][pj];
-          r = rrow[b][e][pos[b][e] - pj];
-        }
-      }
-    };
+    float fa[NP], fr[NP];
     auto prefer = [&](int t) {
-      if constexpr (NB <= 2) {
+      if ((t + 1) * KT <= ctx) {                               // every key cached before the step: no branches, loads side by side
 #pragma unroll
-        for (int x = 0; x < NP; ++x) preference(t, x, fa[x], fr[x]);
+        for (int x = 0; x < NP; ++x) {
+          const int b = x / (SUB * 4), e = x & 1, j = t * KT + x / 4 % SUB * 16 + ((x >> 1) & 1) * 8 + gid;
+          fa[x] = arow[b][e][j];
+          fr[x] = rrow[b][e][max(pos[b][e] - j, 0)];
+          if (pos[b][e] < j) fa[x] = -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < NP; ++x) {
+          const int b = x / (SUB * 4), e = x & 1, j = t * KT + x / 4 % SUB * 16 + ((x >> 1) & 1) * 8 + gid, back = j - ctx;
+          fa[x] = -INFINITY;
+          fr[x] = 0.0f;
+          if (j < u.len) {
+            const int pj = back < 0 || !p.positions ? j : min(max(p.positions[u.first + back], 0), p.Tp - 1);
+            if (pj <= pos[b][e]) {
+              fa[x] = arow[b][e][pj];
+              fr[x] = rrow[b][e][pos[b][e] - pj];
+            }
+          }
+        }
       }
     };
     if (any_frozen) prefer(t_begin);
@@ -497,14 +518,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 #pragma unroll
         for (int x = 0; x < NP; ++x) {
           const int b = x / (SUB * 4), sub = x / 4 % SUB;
-          float a, r;
-          if constexpr (NB <= 2) {
-            a = fa[x];
-            r = fr[x];
-          } else {
-            preference(t, x, a, r);
-          }
-          if (frozen[b][x & 1]) s[b][sub][x & 3] = (a + r) * LOG2E;
+          if (frozen[b][x & 1]) s[b][sub][x & 3] = (fa[x] + fr[x]) * LOG2E;
         }
         if (t + 1 < t_end) prefer(t + 1);
       }
@@ -669,7 +683,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const int row = 8 * b + t2 + odd, at = u.rt * ROWS + row, n = u.first + at / g, h = u.hk * g + at % g;
-        const float ls = l[b][odd], inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+        const float ls = odd ? l[b][1] : l[b][0], ms = odd ? m[b][1] : m[b][0], inv = ls == 0.0f ? 0.0f : 1.0f / ls;
         const int64_t off = static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + (gid & ~1);
 #pragma unroll
         for (int f = 0; f < D / 8; ++f) {
@@ -683,7 +697,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         }
         if (row < rows && gid < 2 && p.LSE) {
           const bool fz = (p.frozen[h >> 5] >> (h & 31)) & 1;
-          p.LSE[static_cast<int64_t>(n) * p.H + h] = fz ? 0.0f : ls == 0.0f ? -INFINITY : (m[b][odd] + log2f(ls)) * LN2;
+          p.LSE[static_cast<int64_t>(n) * p.H + h] = fz ? 0.0f : ls == 0.0f ? -INFINITY : (ms + log2f(ls)) * LN2;
         }
       }
     } else {
@@ -781,7 +795,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 
 template <int D, int NB>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
-  const size_t parts = NB > 2 ? 0 : static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
+  const size_t parts = static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
   p.stages = static_cast<int>(std::min<size_t>(MAX_STAGES, (222 * 1024 - parts) / (W * STAGE)));
   const size_t smem = static_cast<size_t>(W) * p.stages * STAGE + parts + 1024;
   auto kernel = p.o_f32 ? saf_cache_attn_kernel<D, NB, true> : saf_cache_attn_kernel<D, NB, false>;
@@ -792,17 +806,13 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
 template <int D>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
   if (p.max_rows <= 8) return launch<D, 1>(mk, mv, p, num_sms, st);
-  if (p.max_rows <= 16) return launch<D, 2>(mk, mv, p, num_sms, st);
-  return launch<D, 4>(mk, mv, p, num_sms, st);
+  return launch<D, 2>(mk, mv, p, num_sms, st);
 }
 
 }  // namespace
 
-int cache_attn_rows(int max_new, int kv_group) { return std::min(32, max_new * kv_group); }
-// two parts of each block, and with 32-row units two of each warp
-size_t cache_attn_workspace(int max_rows, int D, int num_sms) {
-  return static_cast<size_t>(num_sms) * (max_rows > 16 ? 2 + 2 * W : 2) * part_size(max_rows, D) * sizeof(float);
-}
+int cache_attn_rows(int max_new, int kv_group) { return std::min(16, max_new * kv_group); }
+size_t cache_attn_workspace(int max_rows, int D, int num_sms) { return static_cast<size_t>(num_sms) * 2 * part_size(max_rows, D) * sizeof(float); }
 int cache_attn_box_rows(int D, int page_size) { return D == 64 && page_size % 32 == 0 ? 32 : 16; }
 
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
