@@ -1586,14 +1586,16 @@ int validate_cache(const saf_cache* c) {
   return SAF_OK;
 }
 
-// a pool as [pages][heads][slots][features]; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D read as zero
+// a pool as [pages][heads][feature halves][slots][features]: head dimension 128 in two halves of 64, which one copy of a box brings one
+// after the other, else one; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D (96) read as zero
 int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, int box_rows) {
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
-  cuuint64_t dims[4] = {static_cast<cuuint64_t>(c->D), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->H / kvg),
+  const cuuint64_t halves = c->D == 128 ? 2 : 1;
+  cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->D) / halves, static_cast<cuuint64_t>(c->page_size), halves, static_cast<cuuint64_t>(c->H / kvg),
                         static_cast<cuuint64_t>(c->n_pages)};
-  cuuint64_t gs[3] = {static_cast<cuuint64_t>(strides[2]) * 2, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
-  cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1}, es[4] = {1, 1, 1, 1};
-  return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  cuuint64_t gs[4] = {static_cast<cuuint64_t>(strides[2]) * 2, 128, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
+  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(halves), 1, 1}, es[5] = {1, 1, 1, 1, 1};
+  return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? SAF_OK
              : SAF_ERR_CUDA;
@@ -1689,6 +1691,9 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   if (!frozen_mask_host || c->max_new < 1 || c->max_new > 64 || c->max_len < 1 ||
       c->max_len > static_cast<int64_t>(c->max_pages) * c->page_size)
     return SAF_ERR_INVALID_ARG;
+  const int kvg = c->kv_group > 1 ? c->kv_group : 1;
+  // (tiles are counted in 32 bits)
+  if (cache_attn_tiles(c->max_new, kvg, c->D, c->max_len) > 0x7fffffffLL / (static_cast<int64_t>(c->R) * (c->H / kvg))) return SAF_ERR_UNSUPPORTED;
   CacheAttnParams f{};
   int nf = 0;
   for (int h = 0; h < c->H; ++h)
@@ -1707,7 +1712,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ctx->last_stream = st;
   f.R = c->R; f.N = c->N; f.H = c->H; f.D = c->D; f.Tp = c->Tp;
-  f.kv_group = c->kv_group > 1 ? c->kv_group : 1;
+  f.kv_group = kvg;
   f.page_size = c->page_size; f.n_pages = c->n_pages; f.max_pages = c->max_pages;
   f.max_len = c->max_len; f.max_new = c->max_new;
   f.scale_log2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * 1.4426950408889634f;
@@ -1720,7 +1725,6 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
     bool keys = false;
     for (int h = hk * f.kv_group; h < (hk + 1) * f.kv_group; ++h) keys |= !frozen_mask_host[h];
     if (keys) f.with_keys[hk >> 5] |= 1u << (hk & 31);
-    f.head_weights += keys ? 2 : 1;
   }
   f.max_rows = cache_attn_rows(c->max_new, f.kv_group);
   if ((rc = ensure(ctx->cattn_buf, cache_attn_workspace(f.max_rows, c->D, ctx->num_sms))) ||

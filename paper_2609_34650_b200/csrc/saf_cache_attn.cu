@@ -5,8 +5,7 @@
 //
 // Every key and value is read once for all rows that share it, so DRAM bounds the call unless it is a short one.  A unit is one request,
 // one cached head and up to 8 or 16 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
-// head dimension 64 and 16 above.  The units' tiles, laid end to end and weighed by what they read (2 for keys and values, 1 where all
-// heads of a group are frozen and only values are read), are cut into equal runs, one for each warp of the grid: no run is longer than
+// head dimension 64 and 16 above.  The units' tiles, laid end to end, are cut into equal runs, one for each warp of the grid: no run is longer than
 // another whatever the lengths are, and a single long request fills the GPU like many short ones.  A warp streams its run on its
 // own: it fetches tiles by TMA into a ring of its own, and meets other warps only when the run is over, to join what is left of
 // units that were cut: in shared memory within a block, through L2 between blocks, where the block that arrives last joins the parts in order.
@@ -22,16 +21,17 @@
 namespace saf {
 namespace {
 
-constexpr int W = 8;                // warps of a block
 constexpr int TILE = 4096, STAGE = 2 * TILE;   // a tile of keys or values; both
 constexpr int MAX_STAGES = 4;
 constexpr int SINGLE_TILES = 4;     // tiles a warp up to which a block takes a whole unit where there are no more units than blocks
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-template <int D>
+template <int D, int NB>
 struct Cfg {
-  static constexpr int HALVES = D == 64 ? 1 : 2;              // 64-feature boxes of a tile row (96: zero-filled to 128)
+  static constexpr int HALVES = D == 64 ? 1 : 2;              // 64-feature halves of a tile (96: zero-filled to 128)
+  static constexpr int BOXES = D == 96 ? 2 : 1;               // copies that bring them
   static constexpr int KT = TILE / (HALVES * 128);            // keys of a tile
+  static constexpr int WARPS = NB == 1 ? 12 : 8;              // what the registers allow: 168 a thread for 8 rows, 255 for 16
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -56,27 +56,30 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 
 // Where a run stands: a unit, and its place on the line of all tiles.
 struct Unit {
-  long long start;                  // of the unit's first tile on the line
+  int start;                        // of the unit's first tile on the line
   int r, hk, rt;                    // request, cached head, row tile
   int first, many, len;             // the request's first row, rows that are computed, tokens in its cache
-  int tiles, row_tiles, weight;
+  int tiles, row_tiles;
 };
 
-__device__ __forceinline__ int weight_of(const CacheAttnParams& p, int hk) { return ((p.with_keys[hk >> 5] >> (hk & 31)) & 1) + 1; }
+__device__ __forceinline__ bool has_keys(const CacheAttnParams& p, int hk) { return (p.with_keys[hk >> 5] >> (hk & 31)) & 1; }
 
 template <int KT, int ROWS>
-__device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) {
-  u.first = min(max(p.new_offsets[u.r], 0), p.N);
-  const int last = min(p.new_offsets[u.r + 1], p.N);
-  u.many = min(max(last - u.first, 0), p.max_new);
-  u.len = min(max(p.kv_lens[u.r], 0), p.max_len);
+__device__ __forceinline__ void set_request(const CacheAttnParams& p, Unit& u, int first, int last, int len) {
+  u.first = min(max(first, 0), p.N);
+  u.many = min(max(min(last, p.N) - u.first, 0), p.max_new);
+  u.len = min(max(len, 0), p.max_len);
   u.row_tiles = (u.many * p.kv_group + ROWS - 1) / ROWS;
   u.tiles = max((u.len + KT - 1) / KT, 1);                    // (a request without keys still gets its zeros)
+}
+template <int KT, int ROWS>
+__device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) {
+  set_request<KT, ROWS>(p, u, p.new_offsets[u.r], p.new_offsets[u.r + 1], p.kv_lens[u.r]);
 }
 // The next unit that has rows; u.r = p.R behind the last.
 template <int KT, int ROWS>
 __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
-  u.start += static_cast<long long>(u.weight) * u.tiles;
+  u.start += u.tiles;
   if (++u.rt < u.row_tiles) return;
   u.rt = 0;
   if (++u.hk >= p.H / p.kv_group) {
@@ -86,25 +89,16 @@ __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
       load_request<KT, ROWS>(p, u);
     } while (u.many == 0);
   }
-  u.weight = weight_of(p, u.hk);
 }
 // First tile of the unit at or behind place x, and at most all of them.
-__device__ __forceinline__ int tile_at(const Unit& u, long long x) {
-  const long long d = x - u.start;
-  if (d <= 0) return 0;
-  return static_cast<int>(min((d + u.weight - 1) >> (u.weight - 1), static_cast<long long>(u.tiles)));   // (weight 1 or 2)
-}
-// a / b; the 64-bit division takes several hundred clocks
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
-}
+__device__ __forceinline__ int tile_at(const Unit& u, int x) { return min(max(x - u.start, 0), u.tiles); }
 // `total` places in `runs` runs: the first `more` of them have one place more than the others.
 struct Cut {
-  long long total, runs, each, more;
-  __device__ __forceinline__ long long start(long long id) const { return id >= runs ? total : each * id + min(id, more); }
-  __device__ __forceinline__ int run_of(long long x) const {
-    const long long big = more * (each + 1);
-    return static_cast<int>(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
+  int total, runs, each, more;
+  __device__ __forceinline__ int start(int id) const { return id >= runs ? total : each * id + min(id, more); }
+  __device__ __forceinline__ int run_of(int x) const {
+    const int big = more * (each + 1);
+    return x < big ? x / (each + 1) : more + (x - big) / each;
   }
 };
 
@@ -112,7 +106,7 @@ struct Cut {
 __host__ __device__ constexpr int part_size(int max_rows, int D) { return (max_rows * (D + 2) + 3) / 4 * 4; }
 // What it belongs to:
 struct Part {
-  long long start, last;            // of the unit's first and last tile (start < 0: none)
+  int start, last;                  // of the unit's first and last tile (start < 0: none)
   int first, many, rt, hk;
 };
 
@@ -131,12 +125,6 @@ __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& 
     p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
   }
 }
-
-// Parts of one unit within a block: order[begin .. begin + count), and the blocks that the unit lies in.
-struct Group {
-  Part unit;
-  int begin, count, c_first, c_last;
-};
 
 // Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.
 template <int D, int ROWS, bool GLOBAL, typename At>
@@ -174,25 +162,26 @@ __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, in
 }
 
 template <int D, int NB, bool EXACT>
-__global__ void __launch_bounds__(32 * W, 1)
+__global__ void __launch_bounds__(32 * Cfg<D, NB>::WARPS, 1)
 saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ CacheAttnParams p) {
-  constexpr int HALVES = Cfg<D>::HALVES, KT = Cfg<D>::KT, SUB = KT / 16, NT = 32 * W, ROWS = 8 * NB;
+  constexpr int HALVES = Cfg<D, NB>::HALVES, BOXES = Cfg<D, NB>::BOXES, KT = Cfg<D, NB>::KT, SUB = KT / 16, W = Cfg<D, NB>::WARPS, NT = 32 * W, ROWS = 8 * NB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int stages = p.stages, max_rows = p.max_rows, part_floats = part_size(max_rows, D);
   // [warps][stages] tiles, then a part of each warp's run; at the run's end its ring holds a second one
   auto part_at = [&](int w, int k) -> float* {
-    return k == 0 ? reinterpret_cast<float*>(smem + W * stages * STAGE) + w * part_floats : reinterpret_cast<float*>(smem + w * stages * STAGE);
+    if (k == 1) return reinterpret_cast<float*>(smem + w * stages * STAGE);
+    if (!p.parts_in_smem) return p.workspace + (static_cast<int64_t>(gridDim.x) * 2 + static_cast<int64_t>(blockIdx.x) * W + w) * part_floats;
+    return reinterpret_cast<float*>(smem + W * stages * STAGE) + w * part_floats;
   };
   __shared__ uint64_t full[W][MAX_STAGES];
-  __shared__ Part meta[W][2];
-  __shared__ long long red[W], red_units[W];
-  __shared__ int red_tiles[W], order[2 * W], open_s[2], counts_s[2], arrived_s[2], abort_s;
-  __shared__ Group groups[2 * W];
+  __shared__ int red[W], red_units[W];
+  __shared__ Part open_unit[2];                              // units that go on in other blocks: the block's first, its last
+  __shared__ int red_tiles[W], arrived_s[2], abort_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) abort_s = 0;
   if (lane < stages) mbar_init(&full[warp][lane], 1);
-  if (lane < 2) meta[warp][lane].start = -1;
+  if (threadIdx.x < 2) open_unit[threadIdx.x].start = -1;
   mbar_fence_init();
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&mk);
@@ -202,76 +191,77 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   pdl_launch_dependents();
 
   // ---- the line of all tiles: inclusive sums over the requests (in the ring's memory, before it is used)
-  long long* sums = reinterpret_cast<long long*>(smem);
+  int* sums = reinterpret_cast<int*>(smem);
+  int* firsts = sums + p.R;                                  // [R + 1] and [R]: as in new_offsets and kv_lens
+  int* lens = firsts + p.R + 1;
   const int Hk = p.H / p.kv_group;
   const int per = (p.R + NT - 1) / NT, r0 = min(static_cast<int>(threadIdx.x) * per, p.R), r1 = min(r0 + per, p.R);
-  long long cost = 0, units = 0;
-  int longest = 0;
+  int cost = 0, units = 0, longest = 0;
   for (int r = r0; r < r1; ++r) {
     Unit u;
-    u.r = r;
-    load_request<KT, ROWS>(p, u);
-    cost += static_cast<long long>(u.row_tiles) * u.tiles * p.head_weights;
-    units += static_cast<long long>(u.row_tiles) * Hk;
+    const int first = p.new_offsets[r], last = p.new_offsets[r + 1], len = p.kv_lens[r];
+    firsts[r] = first;
+    if (r == p.R - 1) firsts[p.R] = last;
+    lens[r] = len;
+    set_request<KT, ROWS>(p, u, first, last, len);
+    cost += u.row_tiles * Hk * u.tiles;
+    units += u.row_tiles * Hk;
     if (u.many > 0) longest = max(longest, u.tiles);
     sums[r] = cost;
   }
-  long long scan = cost, scan_units = units;
-#pragma unroll
+  int before = cost, before_units = units;
+#pragma unroll 1
   for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, scan, d), z = __shfl_up_sync(0xffffffffu, scan_units, d);
+    const int y = __shfl_up_sync(0xffffffffu, before, d), z = __shfl_up_sync(0xffffffffu, before_units, d);
     if (lane >= d) {
-      scan += y;
-      scan_units += z;
+      before += y;
+      before_units += z;
     }
   }
   longest = __reduce_max_sync(0xffffffffu, longest);
   if (lane == 31) {
-    red[warp] = scan;
-    red_units[warp] = scan_units;
+    red[warp] = before;
+    red_units[warp] = before_units;
     red_tiles[warp] = longest;
   }
+  before -= cost;
+  before_units -= units;
   __syncthreads();
-  long long before = scan - cost, before_units = scan_units - units;
-  Cut cut{0, 0, 0, 0};
-  long long all_units = 0;
-  for (int w = 0; w < W; ++w) {
-    const long long s = red[w], n = red_units[w];
-    if (w < warp) {
-      before += s;
-      before_units += n;
-    }
-    cut.total += s;
-    all_units += n;
-    longest = max(longest, red_tiles[w]);
-  }
+  // (a lane for each warp)
+  const int wsum = lane < W ? red[lane] : 0, wunits = lane < W ? red_units[lane] : 0;
+  before += __reduce_add_sync(0xffffffffu, lane < warp ? wsum : 0);
+  before_units += __reduce_add_sync(0xffffffffu, lane < warp ? wunits : 0);
+  Cut cut{static_cast<int>(__reduce_add_sync(0xffffffffu, wsum)), 0, 0, 0};
+  const int all_units = __reduce_add_sync(0xffffffffu, wunits);
+  longest = __reduce_max_sync(0xffffffffu, lane < W ? red_tiles[lane] : 0);
   // Few short units: a block each, so that no unit's parts meet through L2.
-  const bool single = all_units <= gridDim.x && longest <= SINGLE_TILES * W;
+  const bool single = all_units <= static_cast<int>(gridDim.x) && longest <= SINGLE_TILES * W;
+  int x0 = blockIdx.x, x1, b0, b1;                           // this warp's run, this block's runs
   if (single) {
-    if (blockIdx.x >= all_units) return;
-    for (int r = r0; r < r1; ++r) {
-      Unit u;
-      u.r = r;
-      load_request<KT, ROWS>(p, u);
-      sums[r] = before_units += static_cast<long long>(u.row_tiles) * Hk;
-    }
+    if (x0 >= all_units) return;
   } else {
-    for (int r = r0; r < r1; ++r) sums[r] += before;
-  }
-  __syncthreads();
-  long long x0 = blockIdx.x, x1, b0, b1;                     // this warp's run, this block's runs
-  if (!single) {
-    // runs of at least two whole tiles
-    cut.runs = max(1ll, min(static_cast<long long>(gridDim.x) * W, (cut.total + 3) / 4));
-    cut.each = quotient(cut.total, cut.runs);
+    // runs of two tiles at least
+    cut.runs = max(1, min(static_cast<int>(gridDim.x) * W, (cut.total + 1) / 2));
+    cut.each = cut.total / cut.runs;
     cut.more = cut.total - cut.each * cut.runs;
-    const long long id = static_cast<long long>(blockIdx.x) * W;
+    const int id = blockIdx.x * W;
     x0 = cut.start(id + warp);
     x1 = cut.start(id + warp + 1);
     b0 = cut.start(id);
     b1 = cut.start(id + W);
     if (b0 >= b1) return;
   }
+  for (int r = r0; r < r1; ++r) {
+    if (single) {
+      Unit u;
+      set_request<KT, ROWS>(p, u, firsts[r], firsts[r + 1], lens[r]);
+      sums[r] = before_units += u.row_tiles * Hk;
+    } else {
+      sums[r] += before;
+    }
+  }
+  __syncthreads();
+  int u_tiles = 0;                                          // of a block's single unit
   Unit u;
   u.r = p.R;
   if (single || x0 < x1) {
@@ -283,29 +273,19 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     }
     u.r = lo;                                               // (x0 is below the total: there is one)
     u.start = lo ? sums[lo - 1] : 0;
-    load_request<KT, ROWS>(p, u);
+    set_request<KT, ROWS>(p, u, firsts[lo], firsts[lo + 1], lens[lo]);
+    const int at = single ? x0 - u.start : (x0 - u.start) / u.tiles;   // number of the unit within its request
+    u.hk = at / u.row_tiles;
+    u.rt = at - u.hk * u.row_tiles;
+    u.start += at * u.tiles;
     if (single) {
-      const int at = static_cast<int>(x0 - u.start);
-      u.hk = at / u.row_tiles;
-      u.rt = at - u.hk * u.row_tiles;
-      u.weight = weight_of(p, u.hk);
+      const int each = u.tiles / W, more = u.tiles - each * W;   // (warps behind the tiles have none)
       u.start = 0;
       b0 = 0;
-      b1 = static_cast<long long>(u.weight) * u.tiles;
-      x0 = u.weight * static_cast<long long>(u.tiles * warp / W);
-      x1 = u.weight * static_cast<long long>(u.tiles * (warp + 1) / W);
+      b1 = u_tiles = u.tiles;
+      x0 = each * warp + min(warp, more);
+      x1 = each * (warp + 1) + min(warp + 1, more);
       if (x0 >= x1) u.r = p.R;
-    } else {
-      u.hk = 0;
-      u.rt = 0;
-      u.weight = weight_of(p, 0);
-      while (u.start + static_cast<long long>(u.weight) * u.tiles * u.row_tiles <= x0) {
-        u.start += static_cast<long long>(u.weight) * u.tiles * u.row_tiles;
-        u.weight = weight_of(p, ++u.hk);
-      }
-      const long long skip = quotient(x0 - u.start, static_cast<long long>(u.weight) * u.tiles);
-      u.rt = static_cast<int>(skip);
-      u.start += skip * u.weight * u.tiles;
     }
   }
   __syncthreads();                                          // the sums have been read: the ring may be filled
@@ -317,7 +297,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 
   // ---- the fetching end of the run: up to `stages` tiles ahead of the multiplying one
   Unit fu = u;
-  int ft = 0, fend = 0, pages_at = 0, page_ids = 0, filled = 0;
+  int ft = 0, fend = 0, pages_at = 0, page_ids = 0, fstage = 0, ahead = 0, fslot = 0;   // ahead: tiles fetched and not yet used
   bool fmore = x0 < x1;                                     // (a block of a single unit: warps without a tile have x0 = x1)
   auto load_pages = [&](int tile) {                          // lane l: page of the 16 keys number tile * SUB + l
     pages_at = tile;
@@ -340,44 +320,54 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       }
     } while (!enter());
     load_pages(ft);
+    fslot = ft * KT % p.page_size;
   };
   if (fmore) {
-    if (enter()) load_pages(ft);
-    else advance();
+    if (enter()) {
+      load_pages(ft);
+      fslot = ft * KT % p.page_size;
+    } else {
+      advance();
+    }
   }
   auto fetch = [&]() {
     if (!fmore) return;
-    const int stage = filled % stages;
     if (ft - pages_at >= 32 / SUB) load_pages(ft);
     int page[SUB];
 #pragma unroll
     for (int c = 0; c < SUB; ++c) page[c] = __shfl_sync(0xffffffffu, page_ids, (ft - pages_at) * SUB + c);
-    const int slot = (ft * KT) % p.page_size;
-    const bool keys = fu.weight == 2;
+    const bool keys = has_keys(p, fu.hk);
     if (lane == 0) {
-      uint8_t* dst = ring + stage * STAGE;
-      uint64_t* bar = &full[warp][stage];
+      uint8_t* dst = ring + fstage * STAGE;
+      uint64_t* bar = &full[warp][fstage];
       // (32 keys: one box where pages hold whole ones, else two, the second only if there are keys in it)
-      const int boxes = SUB == 2 && p.box_rows == 16 && ft * KT + 16 < fu.len ? 2 : 1;
-      const int bytes = boxes * p.box_rows * 128 * HALVES;
+      const bool two = SUB == 2 && p.box_rows == 16 && ft * KT + 16 < fu.len;
+      const int bytes = (two ? 32 : p.box_rows) * 128 * HALVES;
       mbar_expect_tx(bar, keys ? 2 * bytes : bytes);
-      for (int c = 0; c < boxes; ++c) {
-        const int at = c == 0 ? slot : (ft * KT + 16) % p.page_size, id = c == 0 ? page[0] : page[SUB - 1];
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-          if (keys) tma_load_4d(dst + (h + c) * 2048, &mk, bar, 64 * h, at, fu.hk, id);
-          tma_load_4d(dst + TILE + (h + c) * 2048, &mv, bar, 64 * h, at, fu.hk, id);
-        }
+      for (int h = 0; h < BOXES; ++h) {
+        if (keys) tma_load_5d(dst + h * 2048, &mk, bar, 64 * h, fslot, 0, fu.hk, page[0]);
+        tma_load_5d(dst + TILE + h * 2048, &mv, bar, 64 * h, fslot, 0, fu.hk, page[0]);
+      }
+      if (two) {
+        const int at = fslot + 16 == p.page_size ? 0 : fslot + 16;
+        if (keys) tma_load_5d(dst + 2048, &mk, bar, 0, at, 0, fu.hk, page[SUB - 1]);
+        tma_load_5d(dst + TILE + 2048, &mv, bar, 0, at, 0, fu.hk, page[SUB - 1]);
       }
     }
-    ++filled;
+    fstage = fstage + 1 == stages ? 0 : fstage + 1;
+    ++ahead;
+    fslot += KT;
+    while (fslot >= p.page_size) fslot -= p.page_size;
     if (++ft >= fend) advance();
   };
-  for (int s = 0; s < stages; ++s) fetch();
+  bool primed = false;
 
   // ---- the multiplying end
-  int used = 0, n_parts = 0;
+  int stage = 0;
+  uint32_t phase = 0;
   bool alive = true;
+  Part lead{-1, 0, 0, 0, 0, 0};                              // a unit within the block whose parts this warp joins
   while (alive && u.r < p.R && u.start < x1) {
     const int t_begin = tile_at(u, x0), t_end = tile_at(u, x1);
     if (t_begin >= t_end) {
@@ -385,7 +375,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       continue;
     }
     const int ctx = u.len - u.many, rows = min(ROWS, u.many * g - u.rt * ROWS);
-    const bool keys = u.weight == 2;
+    const bool keys = has_keys(p, u.hk);
     // queries, as columns: column gid of each block of eight rows
     uint32_t q[NB][D / 16][2];
     if (keys) {
@@ -400,6 +390,10 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           for (int e = 0; e < 2; ++e) q[b][ks][e] = use ? *reinterpret_cast<const uint32_t*>(Q + ks * 16 + e * 8) : 0u;
       }
     }
+    if (!primed) {                                            // (here, so that the queries and the first pages are fetched side by side)
+      primed = true;
+      for (int s = 0; s < stages; ++s) fetch();
+    }
     // scores and weights: rows 8 b + t2 + e, keys gid and gid + 8 of each 16
     int pos[NB][2];
     bool frozen[NB][2];
@@ -407,7 +401,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     const float* arow[NB][2];
     const float* rrow[NB][2];
     bool any = false;
-    int lead = ROWS;                                          // first frozen row seen
+    int first_frozen = ROWS;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -415,7 +409,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         const int row = 8 * b + t2 + e, at = u.rt * ROWS + min(row, rows - 1), i = at / g, h = u.hk * g + at % g, n = u.first + i;
         frozen[b][e] = (p.frozen[h >> 5] >> (h & 31)) & 1;
         any |= frozen[b][e];
-        if (frozen[b][e]) lead = min(lead, min(row, rows - 1));
+        if (frozen[b][e]) first_frozen = min(first_frozen, min(row, rows - 1));
         mask[b][e] = p.masks ? p.masks[n] : (2ull << i) - 1;   // (i = 63: all)
         pos[b][e] = frozen[b][e] ? (p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + i, 0)) : 0;
         arow[b][e] = p.alpha + static_cast<int64_t>(h) * p.Tp;
@@ -424,7 +418,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     const bool any_frozen = __any_sync(0xffffffffu, any);
     if (any_frozen) {
       // rows of ordinary heads look where the unit's first frozen row looks, so that their loads cost nothing
-      const int first_row = __reduce_min_sync(0xffffffffu, lead);
+      const int first_row = __reduce_min_sync(0xffffffffu, first_frozen);
       const int at = u.rt * ROWS + first_row, h = u.hk * g + at % g, n = u.first + at / g;
       const int ps = p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + at / g, 0);
 #pragma unroll
@@ -480,11 +474,10 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     };
     if (any_frozen) prefer(t_begin);
     for (int t = t_begin; t < t_end; ++t) {
-      const int stage = used % stages;
       const uint32_t ks_addr = ring_s + stage * STAGE, vs_addr = ks_addr + TILE;
       const int j0 = t * KT;
       const bool tail = j0 + KT > ctx;
-      if (!mbar_wait_warp_compact(&full[warp][stage], (used / stages) & 1, wc, 90)) {
+      if (!mbar_wait_warp_compact(&full[warp][stage], phase, wc, 90)) {
         alive = false;
         break;
       }
@@ -497,6 +490,11 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[b][sub][e] = 0.0f;
       if (keys) {
+        float s2[NB][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s2[b][e] = 0.0f;
         const int row = (((lane >> 3) & 1) << 3) + (lane & 7);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
@@ -505,14 +503,17 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             uint32_t a[4];
             ldsm4(ks_addr + (ks >> 2) * 2048 + (sub * 16 + row) * 128 + ((((ks & 3) * 2 + (lane >> 4)) ^ (row & 7)) << 4), a);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) mma16816(s[b][sub], a, q[b][ks][0], q[b][ks][1]);
+            for (int b = 0; b < NB; ++b) {                     // (16 keys: two chains of products)
+              if (SUB == 1 && (ks & 1)) mma16816(s2[b], a, q[b][ks][0], q[b][ks][1]);
+              else mma16816(s[b][sub], a, q[b][ks][0], q[b][ks][1]);
+            }
           }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[b][sub][e] *= p.scale_log2;
+            for (int e = 0; e < 4; ++e) s[b][sub][e] = (SUB == 1 ? s[b][sub][e] + s2[b][e] : s[b][sub][e]) * p.scale_log2;
       }
       if (any_frozen) {
 #pragma unroll
@@ -662,7 +663,11 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       }
       if (tail) fence_proxy_async_smem();                     // (the tile may have been written to: before it is fetched over)
       __syncwarp();
-      ++used;
+      --ahead;
+      if (++stage == stages) {
+        stage = 0;
+        phase ^= 1;
+      }
       fetch();
     }
 #pragma unroll
@@ -671,12 +676,17 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
-    const Part me{u.start, u.start + static_cast<long long>(u.weight) * (u.tiles - 1), u.first, u.many, u.rt, u.hk};
+    const Part me{u.start, u.start + u.tiles - 1, u.first, u.many, u.rt, u.hk};
     if (!alive) {
       // given up: the copies in flight end before the block does (a bounded wait again), nothing is joined
-      for (int i = used; i < filled; ++i)
-        for (int spin = 0; spin < 100000 && !mbar_try_wait(&full[warp][i % stages], (i / stages) & 1); ++spin) {
+      for (; ahead > 0; --ahead) {
+        for (int spin = 0; spin < 100000 && !mbar_try_wait(&full[warp][stage], phase); ++spin) {
         }
+        if (++stage == stages) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
     } else if (t_begin == 0 && t_end == u.tiles) {
       // pairs of lanes exchange, the one taking the even row, the other the odd one, two features each
       const int odd = gid & 1;
@@ -702,7 +712,8 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       }
     } else {
       // the part of a unit that goes on elsewhere: at most two a run, the second when nothing more is fetched
-      float* dst = part_at(warp, n_parts);
+      const int k = x0 >= u.start ? 0 : 1;                     // the run's first unit or a later one, which is its last
+      float* dst = part_at(warp, k);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -717,87 +728,71 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             }
           }
         }
-      if (lane == 0) meta[warp][n_parts] = me;
-      ++n_parts;
+      // who joins: the warp in whose run the unit begins, or, if it lies in several blocks, all of the block
+      if (me.start < b0 || me.last >= b1) {
+        if (lane == 0) open_unit[b0 >= me.start ? 0 : 1] = me;  // (each warp of the unit writes the same)
+      } else if (t_begin == 0) {
+        lead = me;
+      }
     }
     next_unit<KT, ROWS>(p, u);
   }
-  // ---- what is left of cut units, in the order of the runs: warp 0 finds what belongs together, a lane for each part
+  // ---- what is left of cut units, in the order of the runs.  A run's part of a unit lies in its first place if the unit began at or
+  // before the run, else in its second; a block's likewise.
   __syncthreads();
-  if (warp == 0) {
-    const Part mine = lane < 2 * W ? (&meta[0][0])[lane] : Part{-1, 0, 0, 0, 0, 0};
-    const uint32_t below = (1u << lane) - 1;
-    const uint32_t there = __ballot_sync(0xffffffffu, mine.start >= 0);
-    const long long prior = __shfl_sync(0xffffffffu, mine.start, (there & below) ? 31 - __clz(there & below) : 0);
-    const bool leads = mine.start >= 0 && (!(there & below) || prior != mine.start);
-    const uint32_t leaders = __ballot_sync(0xffffffffu, leads);
-    const int at = __popc(there & below);
-    if (mine.start >= 0) order[at] = lane;
-    bool open = false;
-    const int me = __popc(leaders & below);
-    if (leads) {
-      const uint32_t later = leaders & ~below & ~(1u << lane);
-      const int end = later ? __popc(there & ((1u << (__ffs(later) - 1)) - 1)) : __popc(there);
-      Group& gr = groups[me];
-      gr.unit = mine;
-      gr.begin = at;
-      gr.count = end - at;
-      gr.c_first = gr.c_last = 0;
-      if (!single && (mine.start < b0 || mine.last >= b1)) {
-        gr.c_first = cut.run_of(mine.start) / W;
-        gr.c_last = cut.run_of(mine.last) / W;
-        open = true;
-      }
-    }
-    const uint32_t opens = __ballot_sync(0xffffffffu, open);
-    if (open) open_s[__popc(opens & below)] = me;            // (a block's first and last unit at most)
-    if (lane == 0) {
-      counts_s[0] = __popc(leaders);
-      counts_s[1] = __popc(opens);
-    }
-  }
-  __syncthreads();
-  auto part_of = [&](int i) -> const float* { return part_at(i >> 1, i & 1); };
-  const int n_groups = counts_s[0], n_open = counts_s[1];
-  auto slot_of = [&](int block, long long first_place, const Part& unit) {
-    return p.workspace + (static_cast<int64_t>(block) * 2 + (first_place >= unit.start ? 0 : 1)) * part_floats;
+  const int run0 = blockIdx.x * W;
+  auto part_of = [&](int w, const Part& unit) -> const float* { return part_at(w, single || cut.start(run0 + w) >= unit.start ? 0 : 1); };
+  auto slot_of = [&](int block, const Part& unit) {
+    return p.workspace + (static_cast<int64_t>(block) * 2 + (cut.start(block * W) >= unit.start ? 0 : 1)) * part_floats;
   };
-  for (int k = 0; k < n_open; ++k) {
-    const Group& gr = groups[open_s[k]];
-    join<D, ROWS, false>(p, gr.unit, max_rows, gr.count, [&](int i) { return part_of(order[gr.begin + i]); }, slot_of(blockIdx.x, b0, gr.unit), threadIdx.x, NT);
+  for (int k = 0; k < 2; ++k) {
+    const Part unit = open_unit[k];
+    if (unit.start < 0) continue;
+    const int w0 = unit.start <= b0 ? 0 : cut.run_of(unit.start) - run0;
+    const int w1 = unit.last >= b1 ? W - 1 : cut.run_of(unit.last) - run0;
+    join<D, ROWS, false>(p, unit, max_rows, w1 - w0 + 1, [&](int i) { return part_of(w0 + i, unit); }, slot_of(blockIdx.x, unit), threadIdx.x, NT);
   }
-  if (n_open > 0) {
-    __threadfence();
+  const bool any_open = open_unit[0].start >= 0 || open_unit[1].start >= 0;
+  int c_first = 0, c_last = 0;
+  if (any_open) {
     __syncthreads();
-    if (threadIdx.x < n_open) {
-      const Group& gr = groups[open_s[threadIdx.x]];
-      int* counter = p.counters + gr.c_first;
-      const bool last = atomicAdd(counter, 1) == gr.c_last - gr.c_first;
-      arrived_s[threadIdx.x] = last;
+    if (threadIdx.x < 2 && open_unit[threadIdx.x].start >= 0) {
+      const Part& unit = open_unit[threadIdx.x];
+      c_first = cut.run_of(unit.start) / W;
+      c_last = cut.run_of(unit.last) / W;
+      __threadfence();                                        // (the block's parts, which the barrier put before this)
+      int* counter = p.counters + c_first;
+      const bool last = atomicAdd(counter, 1) == c_last - c_first;
       if (last) *counter = 0;
+      arrived_s[threadIdx.x] = last;
       __threadfence();
     }
   }
-  for (int k = 0, turn = 0; k < n_groups; ++k) {
-    const Group& gr = groups[k];
-    if (gr.c_first != gr.c_last) continue;
-    if (turn++ % W == warp) join<D, ROWS, false>(p, gr.unit, max_rows, gr.count, [&](int i) { return part_of(order[gr.begin + i]); }, nullptr, lane, 32);
+  if (lead.start >= 0) {
+    const int members = single ? min(W, u_tiles) : cut.run_of(lead.last) - run0 - warp + 1;
+    join<D, ROWS, false>(p, lead, max_rows, members, [&](int i) { return part_of(warp + i, lead); }, nullptr, lane, 32);
   }
-  if (n_open == 0) return;
+  if (!any_open) return;
   __syncthreads();
-  for (int k = 0; k < n_open; ++k) {
-    if (!arrived_s[k]) continue;
-    const Group& gr = groups[open_s[k]];
-    join<D, ROWS, true>(p, gr.unit, max_rows, gr.c_last - gr.c_first + 1,
-                  [&](int i) { return slot_of(gr.c_first + i, cut.start(static_cast<long long>(gr.c_first + i) * W), gr.unit); }, nullptr, threadIdx.x, NT);
+  for (int k = 0; k < 2; ++k) {
+    const Part unit = open_unit[k];
+    if (unit.start < 0 || !arrived_s[k]) continue;
+    c_first = cut.run_of(unit.start) / W;
+    c_last = cut.run_of(unit.last) / W;
+    join<D, ROWS, true>(p, unit, max_rows, c_last - c_first + 1, [&](int i) { return slot_of(c_first + i, unit); }, nullptr, threadIdx.x, NT);
   }
 }
 
 template <int D, int NB>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
-  const size_t parts = static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
-  p.stages = static_cast<int>(std::min<size_t>(MAX_STAGES, (222 * 1024 - parts) / (W * STAGE)));
-  const size_t smem = static_cast<size_t>(W) * p.stages * STAGE + parts + 1024;
+  constexpr int W = Cfg<D, NB>::WARPS;
+  // two stages a warp at least; the parts of the runs' first units where there is room, else in the workspace
+  const size_t room = 222 * 1024, ring = static_cast<size_t>(W) * STAGE;
+  size_t parts = static_cast<size_t>(W) * part_size(p.max_rows, D) * sizeof(float);
+  p.parts_in_smem = parts + 2 * ring <= room;
+  if (!p.parts_in_smem) parts = 0;
+  p.stages = static_cast<int>(std::min<size_t>(MAX_STAGES, (room - parts) / ring));
+  const size_t smem = p.stages * ring + parts + 1024;
   auto kernel = p.o_f32 ? saf_cache_attn_kernel<D, NB, true> : saf_cache_attn_kernel<D, NB, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
@@ -812,7 +807,11 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
 }  // namespace
 
 int cache_attn_rows(int max_new, int kv_group) { return std::min(16, max_new * kv_group); }
-size_t cache_attn_workspace(int max_rows, int D, int num_sms) { return static_cast<size_t>(num_sms) * 2 * part_size(max_rows, D) * sizeof(float); }
+size_t cache_attn_workspace(int max_rows, int D, int num_sms) { return static_cast<size_t>(num_sms) * (2 + Cfg<64, 1>::WARPS) * part_size(max_rows, D) * sizeof(float); }
+int64_t cache_attn_tiles(int max_new, int kv_group, int D, int max_len) {
+  const int rows = max_new * kv_group, unit = rows <= 8 ? 8 : 16, keys = D == 64 ? 32 : 16;
+  return static_cast<int64_t>((rows + unit - 1) / unit) * ((max_len - 1) / keys + 1);
+}
 int cache_attn_box_rows(int D, int page_size) { return D == 64 && page_size % 32 == 0 ? 32 : 16; }
 
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {

@@ -317,11 +317,10 @@ struct CacheAttnParams {
   void* O; int o_f32;
   float* LSE;
   int max_rows;                     // rows of a unit's part (cache_attn_rows)
-  int head_weights;                 // sum over the cached heads of what a tile reads (1, or 2 with keys)
-  float* workspace;                 // parts of units that lie in two blocks or more: two of each block
+  float* workspace;                 // parts of units that lie in two blocks or more, two of each block; where shared memory lacks room one of each warp
   int* counters;                    // one a block, zero between launches
   int box_rows;                     // slots of a TMA box (cache_attn_box_rows)
-  int stages;                       // set by the launcher
+  int stages, parts_in_smem;        // set by the launcher
   int* status;
   unsigned long long wait_limit_ns;
   uint32_t frozen[CACHE_MAX_HEADS / 32];     // bit per query head
@@ -330,7 +329,8 @@ struct CacheAttnParams {
 int cache_attn_rows(int max_new, int kv_group);
 size_t cache_attn_workspace(int max_rows, int D, int num_sms);
 int cache_attn_box_rows(int D, int page_size);
-// mk, mv: the pools as [pages][heads][slots][features], boxes of p.box_rows slots x 64 features
+int64_t cache_attn_tiles(int max_new, int kv_group, int D, int max_len);   // of a request of the bounds' size, a cached head
+// mk, mv: the pools as [pages][heads][feature halves][slots][features], boxes of p.box_rows slots x 64 features (x 2 halves)
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st);
 
 }  // namespace saf
