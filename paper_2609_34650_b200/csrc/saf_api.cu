@@ -1713,6 +1713,11 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   ctx->last_stream = st;
   f.R = c->R; f.N = c->N; f.H = c->H; f.D = c->D; f.Tp = c->Tp;
   f.kv_group = kvg;
+  f.heads_cached = c->H / kvg;
+  f.group_magic = static_cast<uint32_t>(((1ull << 32) + kvg - 1) / kvg);
+  f.page_shift = -1;
+  for (int b = 0; b < 27; ++b)
+    if (c->page_size == 16 << b) f.page_shift = b;
   f.page_size = c->page_size; f.n_pages = c->n_pages; f.max_pages = c->max_pages;
   f.max_len = c->max_len; f.max_new = c->max_new;
   f.scale_log2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * 1.4426950408889634f;

@@ -59,7 +59,7 @@ struct Unit {
   int start;                        // of the unit's first tile on the line
   int r, hk, rt;                    // request, cached head, row tile
   int first, many, len;             // the request's first row, rows that are computed, tokens in its cache
-  int tiles, row_tiles;
+  int tiles, row_tiles, pitch;      // (pitch: places that a unit takes, 0: its tiles)
 };
 
 __device__ __forceinline__ bool has_keys(const CacheAttnParams& p, int hk) { return (p.with_keys[hk >> 5] >> (hk & 31)) & 1; }
@@ -79,10 +79,10 @@ __device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) 
 // The next unit that has rows; u.r = p.R behind the last.
 template <int KT, int ROWS>
 __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
-  u.start += u.tiles;
+  u.start += u.pitch ? u.pitch : u.tiles;
   if (++u.rt < u.row_tiles) return;
   u.rt = 0;
-  if (++u.hk >= p.H / p.kv_group) {
+  if (++u.hk >= p.heads_cached) {
     u.hk = 0;
     do {
       if (++u.r >= p.R) return;
@@ -102,6 +102,9 @@ struct Cut {
   }
 };
 
+// x / group for x < 2^16
+__device__ __forceinline__ int by_group(const CacheAttnParams& p, int x) { return p.kv_group == 1 ? x : static_cast<int>(__umulhi(x, p.group_magic)); }
+
 // A part of a unit's result: rows x D sums, then maxima, then sums of weights; whole 16-byte words, so that parts lie side by side.
 __host__ __device__ constexpr int part_size(int max_rows, int D) { return (max_rows * (D + 2) + 3) / 4 * 4; }
 // What it belongs to:
@@ -112,7 +115,7 @@ struct Part {
 
 template <int ROWS>
 __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& u, int row, int f, float4 x, float m, float l) {
-  const int g = p.kv_group, at = u.rt * ROWS + row, n = u.first + at / g, h = u.hk * g + at % g;
+  const int g = p.kv_group, at = u.rt * ROWS + row, i = by_group(p, at), n = u.first + i, h = u.hk * g + at - i * g;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;               // (NaN stays NaN)
   const int64_t o = n * p.o_strides[0] + h * p.o_strides[1] + f;
   if (p.o_f32) {
@@ -190,103 +193,103 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   pdl_wait();
   pdl_launch_dependents();
 
-  // ---- the line of all tiles: inclusive sums over the requests (in the ring's memory, before it is used)
+  // ---- the line of all tiles: inclusive sums over each warp's requests (in the ring's memory, before it is used), a warp for
+  // every 32 requests as far as there are warps (the others issue nothing meanwhile)
   int* sums = reinterpret_cast<int*>(smem);
-  int* firsts = sums + p.R;                                  // [R + 1] and [R]: as in new_offsets and kv_lens
+  int* usums = sums + p.R;                                   // of units
+  int* firsts = usums + p.R;                                 // [R + 1] and [R]: as in new_offsets and kv_lens
   int* lens = firsts + p.R + 1;
-  const int Hk = p.H / p.kv_group;
-  const int per = (p.R + NT - 1) / NT, r0 = min(static_cast<int>(threadIdx.x) * per, p.R), r1 = min(r0 + per, p.R);
-  int cost = 0, units = 0, longest = 0;
-  for (int r = r0; r < r1; ++r) {
-    Unit u;
-    const int first = p.new_offsets[r], last = p.new_offsets[r + 1], len = p.kv_lens[r];
-    firsts[r] = first;
-    if (r == p.R - 1) firsts[p.R] = last;
-    lens[r] = len;
-    set_request<KT, ROWS>(p, u, first, last, len);
-    cost += u.row_tiles * Hk * u.tiles;
-    units += u.row_tiles * Hk;
-    if (u.many > 0) longest = max(longest, u.tiles);
-    sums[r] = cost;
-  }
-  int before = cost, before_units = units;
-#pragma unroll 1
-  for (int d = 1; d < 32; d <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, before, d), z = __shfl_up_sync(0xffffffffu, before_units, d);
-    if (lane >= d) {
-      before += y;
-      before_units += z;
-    }
-  }
-  longest = __reduce_max_sync(0xffffffffu, longest);
-  if (lane == 31) {
-    red[warp] = before;
-    red_units[warp] = before_units;
-    red_tiles[warp] = longest;
-  }
-  before -= cost;
-  before_units -= units;
-  __syncthreads();
-  // (a lane for each warp)
-  const int wsum = lane < W ? red[lane] : 0, wunits = lane < W ? red_units[lane] : 0;
-  before += __reduce_add_sync(0xffffffffu, lane < warp ? wsum : 0);
-  before_units += __reduce_add_sync(0xffffffffu, lane < warp ? wunits : 0);
-  Cut cut{static_cast<int>(__reduce_add_sync(0xffffffffu, wsum)), 0, 0, 0};
-  const int all_units = __reduce_add_sync(0xffffffffu, wunits);
-  longest = __reduce_max_sync(0xffffffffu, lane < W ? red_tiles[lane] : 0);
-  // Few short units: a block each, so that no unit's parts meet through L2.
-  const bool single = all_units <= static_cast<int>(gridDim.x) && longest <= SINGLE_TILES * W;
-  int x0 = blockIdx.x, x1, b0, b1;                           // this warp's run, this block's runs
-  if (single) {
-    if (x0 >= all_units) return;
-  } else {
-    // runs of two tiles at least
-    cut.runs = max(1, min(static_cast<int>(gridDim.x) * W, (cut.total + 1) / 2));
-    cut.each = cut.total / cut.runs;
-    cut.more = cut.total - cut.each * cut.runs;
-    const int id = blockIdx.x * W;
-    x0 = cut.start(id + warp);
-    x1 = cut.start(id + warp + 1);
-    b0 = cut.start(id);
-    b1 = cut.start(id + W);
-    if (b0 >= b1) return;
-  }
-  for (int r = r0; r < r1; ++r) {
-    if (single) {
+  const int Hk = p.heads_cached, scanning = min(W, (p.R + 31) >> 5), per = (p.R + 32 * scanning - 1) / (32 * scanning);
+  if (warp < scanning) {
+    const int r0 = min(static_cast<int>(threadIdx.x) * per, p.R), r1 = min(r0 + per, p.R);
+    int cost = 0, units = 0, longest = 0;
+    for (int r = r0; r < r1; ++r) {
       Unit u;
-      set_request<KT, ROWS>(p, u, firsts[r], firsts[r + 1], lens[r]);
-      sums[r] = before_units += u.row_tiles * Hk;
-    } else {
-      sums[r] += before;
+      const int first = p.new_offsets[r], last = p.new_offsets[r + 1], len = p.kv_lens[r];
+      firsts[r] = first;
+      if (r == p.R - 1) firsts[p.R] = last;
+      lens[r] = len;
+      set_request<KT, ROWS>(p, u, first, last, len);
+      cost += u.row_tiles * Hk * u.tiles;
+      units += u.row_tiles * Hk;
+      if (u.many > 0) longest = max(longest, u.tiles);
+      sums[r] = cost;
+      usums[r] = units;
+    }
+    int c = cost, n = units;
+#pragma unroll 1
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, c, d), z = __shfl_up_sync(0xffffffffu, n, d);
+      if (lane >= d) {
+        c += y;
+        n += z;
+      }
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (lane == 31) {
+      red[warp] = c;
+      red_units[warp] = n;
+      red_tiles[warp] = longest;
+    }
+    for (int r = r0; r < r1; ++r) {
+      sums[r] += c - cost;
+      usums[r] += n - units;
     }
   }
   __syncthreads();
-  int u_tiles = 0;                                          // of a block's single unit
+  Cut cut{0, 0, 0, 0};
+  int pitch = 0;                                             // places from one unit to the next, 0: its tiles
+  int chunk_sum = lane < scanning ? red[lane] : 0;
+  {
+    const int chunk_units = lane < scanning ? red_units[lane] : 0;
+    const int units = __reduce_add_sync(0xffffffffu, chunk_units);
+    const int longest = __reduce_max_sync(0xffffffffu, lane < scanning ? red_tiles[lane] : 0);
+    if (units <= static_cast<int>(gridDim.x) && longest <= SINGLE_TILES * W) {
+      // Few short units: a block each, so that no unit's parts meet through L2.
+      cut.each = (longest + W - 1) / W;
+      pitch = cut.each * W;
+      cut.total = units * pitch;
+      cut.runs = units * W;
+      chunk_sum = chunk_units * pitch;
+    } else {
+      // runs of two tiles at least
+      cut.total = __reduce_add_sync(0xffffffffu, chunk_sum);
+      cut.runs = max(1, min(static_cast<int>(gridDim.x) * W, (cut.total + 1) >> 1));
+      cut.each = cut.total / cut.runs;
+      cut.more = cut.total - cut.each * cut.runs;
+    }
+  }
+  const int run0 = blockIdx.x * W;
+  const int x0 = cut.start(run0 + warp), x1 = cut.start(run0 + warp + 1);   // this warp's run
+  const int b0 = cut.start(run0), b1 = cut.start(run0 + W);  // this block's runs
+  if (b0 >= b1) return;
   Unit u;
   u.r = p.R;
-  if (single || x0 < x1) {
-    int lo = 0, hi = p.R;
+  u.pitch = pitch;
+  if (x0 < x1) {
+    int chunk_end = chunk_sum;
+#pragma unroll 1
+    for (int d = 1; d < W; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, chunk_end, d);
+      if (lane >= d) chunk_end += y;
+    }
+    const int chunk = __ffs(__ballot_sync(0xffffffffu, chunk_end > x0)) - 1;   // (x0 is below the total: there is one)
+    const int off = __shfl_sync(0xffffffffu, chunk_end - chunk_sum, chunk);
+    auto sum = [&](int r) { return off + (pitch ? usums[r] * pitch : sums[r]); };
+    int lo = chunk * 32 * per, hi = min(lo + 32 * per, p.R) - 1;
+    const int base = lo;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (sums[mid] > x0) hi = mid;
+      if (sum(mid) > x0) hi = mid;
       else lo = mid + 1;
     }
-    u.r = lo;                                               // (x0 is below the total: there is one)
-    u.start = lo ? sums[lo - 1] : 0;
+    u.r = lo;
+    u.start = lo > base ? sum(lo - 1) : off;
     set_request<KT, ROWS>(p, u, firsts[lo], firsts[lo + 1], lens[lo]);
-    const int at = single ? x0 - u.start : (x0 - u.start) / u.tiles;   // number of the unit within its request
-    u.hk = at / u.row_tiles;
+    const int step = pitch ? pitch : u.tiles, at = (x0 - u.start) / step;   // number of the unit within its request
+    u.hk = u.row_tiles == 1 ? at : at / u.row_tiles;
     u.rt = at - u.hk * u.row_tiles;
-    u.start += at * u.tiles;
-    if (single) {
-      const int each = u.tiles / W, more = u.tiles - each * W;   // (warps behind the tiles have none)
-      u.start = 0;
-      b0 = 0;
-      b1 = u_tiles = u.tiles;
-      x0 = each * warp + min(warp, more);
-      x1 = each * (warp + 1) + min(warp + 1, more);
-      if (x0 >= x1) u.r = p.R;
-    }
+    u.start += at * step;
   }
   __syncthreads();                                          // the sums have been read: the ring may be filled
 
@@ -298,12 +301,12 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   // ---- the fetching end of the run: up to `stages` tiles ahead of the multiplying one
   Unit fu = u;
   int ft = 0, fend = 0, pages_at = 0, page_ids = 0, fstage = 0, ahead = 0, fslot = 0;   // ahead: tiles fetched and not yet used
-  bool fmore = x0 < x1;                                     // (a block of a single unit: warps without a tile have x0 = x1)
+  bool fmore = x0 < x1;                                     // (a run may still have no tile, behind the end of a unit that has a block to itself)
   auto load_pages = [&](int tile) {                          // lane l: page of the 16 keys number tile * SUB + l
     pages_at = tile;
     const int c = tile * SUB + lane;
     int id = 0;
-    if (c * 16 < max(fu.len, 1)) id = p.block_table[static_cast<int64_t>(fu.r) * p.max_pages + c * 16 / p.page_size];
+    if (c * 16 < max(fu.len, 1)) id = p.block_table[static_cast<int64_t>(fu.r) * p.max_pages + (p.page_shift >= 0 ? c >> p.page_shift : c / (p.page_size >> 4))];
     page_ids = min(max(id, 0), p.n_pages - 1);
   };
   auto enter = [&]() {                                       // false: the unit has no tile in the run
@@ -320,12 +323,12 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       }
     } while (!enter());
     load_pages(ft);
-    fslot = ft * KT % p.page_size;
+    fslot = p.page_shift >= 0 ? (ft * KT) & (p.page_size - 1) : ft * KT % p.page_size;
   };
   if (fmore) {
     if (enter()) {
       load_pages(ft);
-      fslot = ft * KT % p.page_size;
+      fslot = p.page_shift >= 0 ? (ft * KT) & (p.page_size - 1) : ft * KT % p.page_size;
     } else {
       advance();
     }
@@ -381,9 +384,9 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     if (keys) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const int at = u.rt * ROWS + min(8 * b + gid, rows - 1), h = u.hk * g + at % g;
+        const int at = u.rt * ROWS + min(8 * b + gid, rows - 1), i = by_group(p, at), h = u.hk * g + at - i * g;
         const bool use = 8 * b + gid < rows && !((p.frozen[h >> 5] >> (h & 31)) & 1);
-        const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(u.first + at / g) * p.q_strides[0] + h * p.q_strides[1] + t2;
+        const __nv_bfloat16* Q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(u.first + i) * p.q_strides[0] + h * p.q_strides[1] + t2;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
@@ -406,7 +409,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int row = 8 * b + t2 + e, at = u.rt * ROWS + min(row, rows - 1), i = at / g, h = u.hk * g + at % g, n = u.first + i;
+        const int row = 8 * b + t2 + e, at = u.rt * ROWS + min(row, rows - 1), i = by_group(p, at), h = u.hk * g + at - i * g, n = u.first + i;
         frozen[b][e] = (p.frozen[h >> 5] >> (h & 31)) & 1;
         any |= frozen[b][e];
         if (frozen[b][e]) first_frozen = min(first_frozen, min(row, rows - 1));
@@ -419,8 +422,8 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     if (any_frozen) {
       // rows of ordinary heads look where the unit's first frozen row looks, so that their loads cost nothing
       const int first_row = __reduce_min_sync(0xffffffffu, first_frozen);
-      const int at = u.rt * ROWS + first_row, h = u.hk * g + at % g, n = u.first + at / g;
-      const int ps = p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + at / g, 0);
+      const int at = u.rt * ROWS + first_row, i = by_group(p, at), h = u.hk * g + at - i * g, n = u.first + i;
+      const int ps = p.positions ? min(max(p.positions[n], 0), p.Tp - 1) : max(ctx + i, 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -692,7 +695,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       const int odd = gid & 1;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const int row = 8 * b + t2 + odd, at = u.rt * ROWS + row, n = u.first + at / g, h = u.hk * g + at % g;
+        const int row = 8 * b + t2 + odd, at = u.rt * ROWS + row, i = by_group(p, at), n = u.first + i, h = u.hk * g + at - i * g;
         const float ls = odd ? l[b][1] : l[b][0], ms = odd ? m[b][1] : m[b][0], inv = ls == 0.0f ? 0.0f : 1.0f / ls;
         const int64_t off = static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + (gid & ~1);
 #pragma unroll
@@ -740,8 +743,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   // ---- what is left of cut units, in the order of the runs.  A run's part of a unit lies in its first place if the unit began at or
   // before the run, else in its second; a block's likewise.
   __syncthreads();
-  const int run0 = blockIdx.x * W;
-  auto part_of = [&](int w, const Part& unit) -> const float* { return part_at(w, single || cut.start(run0 + w) >= unit.start ? 0 : 1); };
+  auto part_of = [&](int w, const Part& unit) -> const float* { return part_at(w, cut.start(run0 + w) >= unit.start ? 0 : 1); };
   auto slot_of = [&](int block, const Part& unit) {
     return p.workspace + (static_cast<int64_t>(block) * 2 + (cut.start(block * W) >= unit.start ? 0 : 1)) * part_floats;
   };
@@ -769,7 +771,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     }
   }
   if (lead.start >= 0) {
-    const int members = single ? min(W, u_tiles) : cut.run_of(lead.last) - run0 - warp + 1;
+    const int members = cut.run_of(lead.last) - run0 - warp + 1;
     join<D, ROWS, false>(p, lead, max_rows, members, [&](int i) { return part_of(warp + i, lead); }, nullptr, lane, 32);
   }
   if (!any_open) return;

@@ -307,6 +307,9 @@ cudaError_t launch_cache_plan(const CachePlanParams& p, int num_sms, cudaStream_
 constexpr int CACHE_MAX_HEADS = 1024;
 struct CacheAttnParams {
   int R, N, H, kv_group, D, Tp;
+  int heads_cached;                 // H / kv_group
+  uint32_t group_magic;             // ceil(2^32 / kv_group)
+  int page_shift;                   // log2(page_size / 16), -1 if that is no power of two
   int page_size, n_pages, max_pages, max_len, max_new;
   float scale_log2;
   const void* q;
