@@ -1587,14 +1587,14 @@ int validate_cache(const saf_cache* c) {
 }
 
 // a pool as [pages][heads][feature halves][slots][features]: head dimension 128 in two halves of 64, which one copy of a box brings one
-// after the other, else one; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D (96) read as zero
-int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, int box_rows) {
+// after the other, or as one; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D read as zero
+int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, const CacheAttnForm& form) {
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
-  const cuuint64_t halves = c->D == 128 ? 2 : 1;
+  const cuuint64_t halves = form.halves;
   cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->D) / halves, static_cast<cuuint64_t>(c->page_size), halves, static_cast<cuuint64_t>(c->H / kvg),
                         static_cast<cuuint64_t>(c->n_pages)};
   cuuint64_t gs[4] = {static_cast<cuuint64_t>(strides[2]) * 2, 128, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
-  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(halves), 1, 1}, es[5] = {1, 1, 1, 1, 1};
+  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(form.box_rows), static_cast<cuuint32_t>(halves), 1, 1}, es[5] = {1, 1, 1, 1, 1};
   return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? SAF_OK
@@ -1693,7 +1693,8 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
     return SAF_ERR_INVALID_ARG;
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
   // (tiles are counted in 32 bits)
-  if (cache_attn_tiles(c->max_new, kvg, c->D, c->max_len) > 0x7fffffffLL / (static_cast<int64_t>(c->R) * (c->H / kvg))) return SAF_ERR_UNSUPPORTED;
+  const CacheAttnForm form = cache_attn_form(c->max_new, kvg, c->D, c->page_size, c->max_len, c->o_dtype == SAF_F32, ctx->num_sms);
+  if (form.tiles > 0x7fffffffLL / (static_cast<int64_t>(c->R) * (c->H / kvg))) return SAF_ERR_UNSUPPORTED;
   CacheAttnParams f{};
   int nf = 0;
   for (int h = 0; h < c->H; ++h)
@@ -1731,18 +1732,21 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
     for (int h = hk * f.kv_group; h < (hk + 1) * f.kv_group; ++h) keys |= !frozen_mask_host[h];
     if (keys) f.with_keys[hk >> 5] |= 1u << (hk & 31);
   }
-  f.max_rows = cache_attn_rows(c->max_new, f.kv_group);
-  if ((rc = ensure(ctx->cattn_buf, cache_attn_workspace(f.max_rows, c->D, ctx->num_sms))) ||
-      (rc = ensure(ctx->cattn_counters, ctx->num_sms * sizeof(int))) || (rc = zero_if_fresh(ctx->cattn_counters, st)))
+  f.max_rows = form.max_rows;
+  f.tile_tokens = form.tile_tokens;
+  f.box_rows = form.box_rows;
+  f.v = v_cache;
+  for (int i = 0; i < 3; ++i) f.v_strides[i] = c->v_strides[i];
+  if ((rc = ensure(ctx->cattn_buf, form.parts * form.part_bytes)) || (rc = ensure(ctx->cattn_counters, form.blocks * sizeof(int))) ||
+      (rc = zero_if_fresh(ctx->cattn_counters, st)))
     return rc;
   f.workspace = static_cast<float*>(ctx->cattn_buf.ptr);
   f.counters = static_cast<int*>(ctx->cattn_counters.ptr);
   f.status = ctx->status_dev;
   f.wait_limit_ns = ctx->wait_limit_ns;
   CUtensorMap mk, mv;
-  f.box_rows = cache_attn_box_rows(c->D, c->page_size);
-  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, f.box_rows)) ||
-      (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, f.box_rows)))
+  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, form)) ||
+      (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, form)))
     return rc;
   f.block_table = block_table; f.new_offsets = new_offsets; f.kv_lens = kv_lens; f.positions = positions;
   f.masks = reinterpret_cast<const unsigned long long*>(tree_masks);
@@ -1750,7 +1754,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.O = O; f.o_f32 = c->o_dtype == SAF_F32 ? 1 : 0;
   f.LSE = LSE;
   ScopedTimer timer(ctx, SAF_KERNEL_CACHE_ATTN, st);
-  return launch_cache_attn(mk, mv, f, ctx->num_sms, st) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
+  return (form.wide ? launch_cache_wide(mk, mv, f, ctx->num_sms, st) : launch_cache_attn(mk, mv, f, ctx->num_sms, st)) == cudaSuccess ? SAF_OK : SAF_ERR_CUDA;
 }
 
 int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out) {

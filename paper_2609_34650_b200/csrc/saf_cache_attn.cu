@@ -12,11 +12,7 @@
 // The products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that keys and features fill the 16-row side of the matrix
 // instructions and the few rows of a step their 8-column side (with rows on the 16-row side the kernel issued twice the
 // instructions, which bound it at 550 a tile of 16 keys).
-#include "ptx.cuh"
-#include "saf_internal.h"
-
-#include <algorithm>
-#include <cuda_bf16.h>
+#include "saf_cache_attn.cuh"
 
 namespace saf {
 namespace {
@@ -24,7 +20,6 @@ namespace {
 constexpr int TILE = 4096, STAGE = 2 * TILE;   // a tile of keys or values; both
 constexpr int MAX_STAGES = 4;
 constexpr int SINGLE_TILES = 4;     // tiles a warp up to which a block takes a whole unit where there are no more units than blocks
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <int D, int NB>
 struct Cfg {
@@ -54,116 +49,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-// Where a run stands: a unit, and its place on the line of all tiles.
-struct Unit {
-  int start;                        // of the unit's first tile on the line
-  int r, hk, rt;                    // request, cached head, row tile
-  int first, many, len;             // the request's first row, rows that are computed, tokens in its cache
-  int tiles, row_tiles, pitch;      // (pitch: places that a unit takes, 0: its tiles)
-};
-
-__device__ __forceinline__ bool has_keys(const CacheAttnParams& p, int hk) { return (p.with_keys[hk >> 5] >> (hk & 31)) & 1; }
-
-template <int KT, int ROWS>
-__device__ __forceinline__ void set_request(const CacheAttnParams& p, Unit& u, int first, int last, int len) {
-  u.first = min(max(first, 0), p.N);
-  u.many = min(max(min(last, p.N) - u.first, 0), p.max_new);
-  u.len = min(max(len, 0), p.max_len);
-  u.row_tiles = (u.many * p.kv_group + ROWS - 1) / ROWS;
-  u.tiles = max((u.len + KT - 1) / KT, 1);                    // (a request without keys still gets its zeros)
-}
-template <int KT, int ROWS>
-__device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) {
-  set_request<KT, ROWS>(p, u, p.new_offsets[u.r], p.new_offsets[u.r + 1], p.kv_lens[u.r]);
-}
-// The next unit that has rows; u.r = p.R behind the last.
-template <int KT, int ROWS>
-__device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
-  u.start += u.pitch ? u.pitch : u.tiles;
-  if (++u.rt < u.row_tiles) return;
-  u.rt = 0;
-  if (++u.hk >= p.heads_cached) {
-    u.hk = 0;
-    do {
-      if (++u.r >= p.R) return;
-      load_request<KT, ROWS>(p, u);
-    } while (u.many == 0);
-  }
-}
-// First tile of the unit at or behind place x, and at most all of them.
-__device__ __forceinline__ int tile_at(const Unit& u, int x) { return min(max(x - u.start, 0), u.tiles); }
-// `total` places in `runs` runs: the first `more` of them have one place more than the others.
-struct Cut {
-  int total, runs, each, more;
-  __device__ __forceinline__ int start(int id) const { return id >= runs ? total : each * id + min(id, more); }
-  __device__ __forceinline__ int run_of(int x) const {
-    const int big = more * (each + 1);
-    return x < big ? x / (each + 1) : more + (x - big) / each;
-  }
-};
-
-// x / group for x < 2^16
-__device__ __forceinline__ int by_group(const CacheAttnParams& p, int x) { return p.kv_group == 1 ? x : static_cast<int>(__umulhi(x, p.group_magic)); }
-
-// A part of a unit's result: rows x D sums, then maxima, then sums of weights; whole 16-byte words, so that parts lie side by side.
-__host__ __device__ constexpr int part_size(int max_rows, int D) { return (max_rows * (D + 2) + 3) / 4 * 4; }
-// What it belongs to:
-struct Part {
-  int start, last;                  // of the unit's first and last tile (start < 0: none)
-  int first, many, rt, hk;
-};
-
-template <int ROWS>
-__device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& u, int row, int f, float4 x, float m, float l) {
-  const int g = p.kv_group, at = u.rt * ROWS + row, i = by_group(p, at), n = u.first + i, h = u.hk * g + at - i * g;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;               // (NaN stays NaN)
-  const int64_t o = n * p.o_strides[0] + h * p.o_strides[1] + f;
-  if (p.o_f32) {
-    *reinterpret_cast<float4*>(static_cast<float*>(p.O) + o) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-  } else {
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.O) + o) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
-  }
-  if (f == 0 && p.LSE) {
-    const bool frozen = (p.frozen[h >> 5] >> (h & 31)) & 1;
-    p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
-  }
-}
-
-// Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.
-template <int D, int ROWS, bool GLOBAL, typename At>
-__device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, int max_rows, int members, At at, float* dst, int tid, int nthr) {
-  const int rows = min(ROWS, u.many * p.kv_group - u.rt * ROWS);
-  for (int e = tid; e < rows * (D / 4); e += nthr) {
-    const int row = e / (D / 4), f = (e - row * (D / 4)) * 4;
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < members; ++i) {
-      const float* s = at(i) + max_rows * D + row;
-      m = fmaxf(m, GLOBAL ? __ldcg(s) : *s);
-    }
-    const float base = m == -INFINITY ? 0.0f : m;
-    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int i = 0; i < members; ++i) {
-      const float* s = at(i);
-      const float* q = s + max_rows * D + row;
-      const float4 v = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(s + row * D + f)) : *reinterpret_cast<const float4*>(s + row * D + f);
-      const float w = ex2_approx((GLOBAL ? __ldcg(q) : *q) - base);
-      l += w * (GLOBAL ? __ldcg(q + max_rows) : q[max_rows]);
-      x.x += w * v.x; x.y += w * v.y; x.z += w * v.z; x.w += w * v.w;
-    }
-    if (dst) {
-      *reinterpret_cast<float4*>(dst + row * D + f) = x;
-      if (f == 0) {
-        dst[max_rows * D + row] = m;
-        dst[max_rows * (D + 1) + row] = l;
-      }
-    } else {
-      write_row<ROWS>(p, u, row, f, x, m, l);
-    }
-  }
-}
-
 template <int D, int NB, bool EXACT>
 __global__ void __launch_bounds__(32 * Cfg<D, NB>::WARPS, 1)
 saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ CacheAttnParams p) {
@@ -178,9 +63,8 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     return reinterpret_cast<float*>(smem + W * stages * STAGE) + w * part_floats;
   };
   __shared__ uint64_t full[W][MAX_STAGES];
-  __shared__ int red[W], red_units[W];
   __shared__ Part open_unit[2];                              // units that go on in other blocks: the block's first, its last
-  __shared__ int red_tiles[W], arrived_s[2], abort_s;
+  __shared__ int red[3][W], arrived_s[2], abort_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) abort_s = 0;
   if (lane < stages) mbar_init(&full[warp][lane], 1);
@@ -193,104 +77,13 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   pdl_wait();
   pdl_launch_dependents();
 
-  // ---- the line of all tiles: inclusive sums over each warp's requests (in the ring's memory, before it is used), a warp for
-  // every 32 requests as far as there are warps (the others issue nothing meanwhile)
-  int* sums = reinterpret_cast<int*>(smem);
-  int* usums = sums + p.R;                                   // of units
-  int* firsts = usums + p.R;                                 // [R + 1] and [R]: as in new_offsets and kv_lens
-  int* lens = firsts + p.R + 1;
-  const int Hk = p.heads_cached, scanning = min(W, (p.R + 31) >> 5), per = (p.R + 32 * scanning - 1) / (32 * scanning);
-  if (warp < scanning) {
-    const int r0 = min(static_cast<int>(threadIdx.x) * per, p.R), r1 = min(r0 + per, p.R);
-    int cost = 0, units = 0, longest = 0;
-    for (int r = r0; r < r1; ++r) {
-      Unit u;
-      const int first = p.new_offsets[r], last = p.new_offsets[r + 1], len = p.kv_lens[r];
-      firsts[r] = first;
-      if (r == p.R - 1) firsts[p.R] = last;
-      lens[r] = len;
-      set_request<KT, ROWS>(p, u, first, last, len);
-      cost += u.row_tiles * Hk * u.tiles;
-      units += u.row_tiles * Hk;
-      if (u.many > 0) longest = max(longest, u.tiles);
-      sums[r] = cost;
-      usums[r] = units;
-    }
-    int c = cost, n = units;
-#pragma unroll 1
-    for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, c, d), z = __shfl_up_sync(0xffffffffu, n, d);
-      if (lane >= d) {
-        c += y;
-        n += z;
-      }
-    }
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    if (lane == 31) {
-      red[warp] = c;
-      red_units[warp] = n;
-      red_tiles[warp] = longest;
-    }
-    for (int r = r0; r < r1; ++r) {
-      sums[r] += c - cost;
-      usums[r] += n - units;
-    }
-  }
-  __syncthreads();
-  Cut cut{0, 0, 0, 0};
-  int pitch = 0;                                             // places from one unit to the next, 0: its tiles
-  int chunk_sum = lane < scanning ? red[lane] : 0;
-  {
-    const int chunk_units = lane < scanning ? red_units[lane] : 0;
-    const int units = __reduce_add_sync(0xffffffffu, chunk_units);
-    const int longest = __reduce_max_sync(0xffffffffu, lane < scanning ? red_tiles[lane] : 0);
-    if (units <= static_cast<int>(gridDim.x) && longest <= SINGLE_TILES * W) {
-      // Few short units: a block each, so that no unit's parts meet through L2.
-      cut.each = (longest + W - 1) / W;
-      pitch = cut.each * W;
-      cut.total = units * pitch;
-      cut.runs = units * W;
-      chunk_sum = chunk_units * pitch;
-    } else {
-      // runs of two tiles at least
-      cut.total = __reduce_add_sync(0xffffffffu, chunk_sum);
-      cut.runs = max(1, min(static_cast<int>(gridDim.x) * W, (cut.total + 1) >> 1));
-      cut.each = cut.total / cut.runs;
-      cut.more = cut.total - cut.each * cut.runs;
-    }
-  }
-  const int run0 = blockIdx.x * W;
-  const int x0 = cut.start(run0 + warp), x1 = cut.start(run0 + warp + 1);   // this warp's run
-  const int b0 = cut.start(run0), b1 = cut.start(run0 + W);  // this block's runs
-  if (b0 >= b1) return;
+  // ---- this warp's run (the ring's memory is not used yet)
+  Cut cut;
   Unit u;
-  u.r = p.R;
-  u.pitch = pitch;
-  if (x0 < x1) {
-    int chunk_end = chunk_sum;
-#pragma unroll 1
-    for (int d = 1; d < W; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, chunk_end, d);
-      if (lane >= d) chunk_end += y;
-    }
-    const int chunk = __ffs(__ballot_sync(0xffffffffu, chunk_end > x0)) - 1;   // (x0 is below the total: there is one)
-    const int off = __shfl_sync(0xffffffffu, chunk_end - chunk_sum, chunk);
-    auto sum = [&](int r) { return off + (pitch ? usums[r] * pitch : sums[r]); };
-    int lo = chunk * 32 * per, hi = min(lo + 32 * per, p.R) - 1;
-    const int base = lo;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (sum(mid) > x0) hi = mid;
-      else lo = mid + 1;
-    }
-    u.r = lo;
-    u.start = lo > base ? sum(lo - 1) : off;
-    set_request<KT, ROWS>(p, u, firsts[lo], firsts[lo + 1], lens[lo]);
-    const int step = pitch ? pitch : u.tiles, at = (x0 - u.start) / step;   // number of the unit within its request
-    u.hk = u.row_tiles == 1 ? at : at / u.row_tiles;
-    u.rt = at - u.hk * u.row_tiles;
-    u.start += at * step;
-  }
+  int x0, x1;
+  place_run<KT, ROWS, W, W, SINGLE_TILES>(p, smem, red, warp, cut, x0, x1, u);
+  const int run0 = blockIdx.x * W, b0 = cut.start(run0), b1 = cut.start(run0 + W);   // the block's runs
+  if (b0 >= b1) return;
   __syncthreads();                                          // the sums have been read: the ring may be filled
 
   uint8_t* ring = smem + warp * stages * STAGE;
@@ -808,13 +601,23 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
 
 }  // namespace
 
-int cache_attn_rows(int max_new, int kv_group) { return std::min(16, max_new * kv_group); }
-size_t cache_attn_workspace(int max_rows, int D, int num_sms) { return static_cast<size_t>(num_sms) * (2 + Cfg<64, 1>::WARPS) * part_size(max_rows, D) * sizeof(float); }
-int64_t cache_attn_tiles(int max_new, int kv_group, int D, int max_len) {
-  const int rows = max_new * kv_group, unit = rows <= 8 ? 8 : 16, keys = D == 64 ? 32 : 16;
-  return static_cast<int64_t>((rows + unit - 1) / unit) * ((max_len - 1) / keys + 1);
+CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32, int num_sms) {
+  const int rows = max_new * kv_group;
+  // (fp32 output needs weights of 24 bits, three terms of which the wide form's TMEM has no room for)
+  if (rows > 16 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len, num_sms);
+  CacheAttnForm f;
+  f.wide = false;
+  f.tile_tokens = 0;
+  f.max_rows = std::min(16, rows);
+  f.halves = D == 128 ? 2 : 1;
+  f.box_rows = D == 64 && page_size % 32 == 0 ? 32 : 16;
+  f.blocks = num_sms;
+  f.parts = num_sms * (2 + Cfg<64, 1>::WARPS);
+  f.part_bytes = part_size(f.max_rows, D) * sizeof(float);
+  const int unit = rows <= 8 ? 8 : 16, keys = D == 64 ? 32 : 16;
+  f.tiles = static_cast<int64_t>((rows - 1) / unit + 1) * ((max_len - 1) / keys + 1);
+  return f;
 }
-int cache_attn_box_rows(int D, int page_size) { return D == 64 && page_size % 32 == 0 ? 32 : 16; }
 
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {
   if (p.D == 64) return launch<64>(mk, mv, p, num_sms, st);

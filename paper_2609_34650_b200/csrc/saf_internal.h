@@ -312,29 +312,37 @@ struct CacheAttnParams {
   int page_shift;                   // log2(page_size / 16), -1 if that is no power of two
   int page_size, n_pages, max_pages, max_len, max_new;
   float scale_log2;
-  const void* q;
-  int64_t q_strides[2], o_strides[2];
+  const void* q; const void* v;     // (the pools are read through their maps, but for a few values)
+  int64_t q_strides[2], o_strides[2], v_strides[3];
   const int* block_table; const int* new_offsets; const int* kv_lens; const int* positions;
   const unsigned long long* masks;
   const float* alpha; const float* rho;
   void* O; int o_f32;
   float* LSE;
-  int max_rows;                     // rows of a unit's part (cache_attn_rows)
+  int max_rows, tile_tokens;        // CacheAttnForm
   float* workspace;                 // parts of units that lie in two blocks or more, two of each block; where shared memory lacks room one of each warp
   int* counters;                    // one a block, zero between launches
-  int box_rows;                     // slots of a TMA box (cache_attn_box_rows)
+  int box_rows;                     // CacheAttnForm
   int stages, parts_in_smem;        // set by the launcher
   int* status;
   unsigned long long wait_limit_ns;
   uint32_t frozen[CACHE_MAX_HEADS / 32];     // bit per query head
   uint32_t with_keys[CACHE_MAX_HEADS / 32];  // bit per cached head: some query head of its group is ordinary
 };
-int cache_attn_rows(int max_new, int kv_group);
-size_t cache_attn_workspace(int max_rows, int D, int num_sms);
-int cache_attn_box_rows(int D, int page_size);
-int64_t cache_attn_tiles(int max_new, int kv_group, int D, int max_len);   // of a request of the bounds' size, a cached head
-// mk, mv: the pools as [pages][heads][feature halves][slots][features], boxes of p.box_rows slots x 64 features (x 2 halves)
+// How a call runs: units of up to 16 rows, a run a warp (saf_cache_attn.cu), or of up to 128, a run a block, on tcgen05 (saf_cache_wide.cu).
+struct CacheAttnForm {
+  bool wide;
+  int tile_tokens;                  // wide: new tokens of a unit
+  int max_rows;                     // rows of a unit's part
+  int halves, box_rows;             // of the pools' tensor maps: [pages][heads][feature halves][slots][features], boxes of box_rows slots x 64 features
+  int blocks, parts;                // counters, and parts in the workspace
+  size_t part_bytes;
+  int64_t tiles;                    // of a request of the bounds' size, a cached head
+};
+CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32, int num_sms);
+CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, int max_len, int num_sms);
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st);
+cudaError_t launch_cache_wide(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnParams& p, int num_sms, cudaStream_t st);
 
 }  // namespace saf
 
