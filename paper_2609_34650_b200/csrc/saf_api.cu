@@ -1588,13 +1588,13 @@ int validate_cache(const saf_cache* c) {
 
 // a pool as [pages][heads][feature halves][slots][features]: head dimension 128 in two halves of 64, which one copy of a box brings one
 // after the other, or as one; box = 64 features x box_rows slots, 128-byte swizzle, features beyond D read as zero
-int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, const CacheAttnForm& form) {
+int make_pool_map(saf_ctx* ctx, CUtensorMap* out, const void* base, const saf_cache* c, const int64_t* strides, int halves_of, int box_rows) {
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
-  const cuuint64_t halves = form.halves;
+  const cuuint64_t halves = halves_of;
   cuuint64_t dims[5] = {static_cast<cuuint64_t>(c->D) / halves, static_cast<cuuint64_t>(c->page_size), halves, static_cast<cuuint64_t>(c->H / kvg),
                         static_cast<cuuint64_t>(c->n_pages)};
   cuuint64_t gs[4] = {static_cast<cuuint64_t>(strides[2]) * 2, 128, static_cast<cuuint64_t>(strides[1]) * 2, static_cast<cuuint64_t>(strides[0]) * 2};
-  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(form.box_rows), static_cast<cuuint32_t>(halves), 1, 1}, es[5] = {1, 1, 1, 1, 1};
+  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(halves), 1, 1}, es[5] = {1, 1, 1, 1, 1};
   return ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, gs, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? SAF_OK
@@ -1745,8 +1745,8 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.status = ctx->status_dev;
   f.wait_limit_ns = ctx->wait_limit_ns;
   CUtensorMap mk, mv;
-  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, form)) ||
-      (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, form)))
+  if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, form.halves_v, form.box_rows)) ||
+      (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, form.halves_k, form.box_rows)))
     return rc;
   f.block_table = block_table; f.new_offsets = new_offsets; f.kv_lens = kv_lens; f.positions = positions;
   f.masks = reinterpret_cast<const unsigned long long*>(tree_masks);

@@ -609,7 +609,7 @@ CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, i
   f.wide = false;
   f.tile_tokens = 0;
   f.max_rows = std::min(16, rows);
-  f.halves = D == 128 ? 2 : 1;
+  f.halves_k = f.halves_v = D == 128 ? 2 : 1;
   f.box_rows = D == 64 && page_size % 32 == 0 ? 32 : 16;
   f.blocks = num_sms;
   f.parts = num_sms * (2 + Cfg<64, 1>::WARPS);

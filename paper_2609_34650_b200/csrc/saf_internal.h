@@ -334,7 +334,7 @@ struct CacheAttnForm {
   bool wide;
   int tile_tokens;                  // wide: new tokens of a unit
   int max_rows;                     // rows of a unit's part
-  int halves, box_rows;             // of the pools' tensor maps: [pages][heads][feature halves][slots][features], boxes of box_rows slots x 64 features
+  int halves_k, halves_v, box_rows; // of the pools' tensor maps: [pages][heads][feature halves][slots][features], boxes of box_rows slots x 64 features
   int blocks, parts;                // counters, and parts in the workspace
   size_t part_bytes;
   int64_t tiles;                    // of a request of the bounds' size, a cached head
