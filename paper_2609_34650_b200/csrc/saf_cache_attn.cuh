@@ -108,37 +108,65 @@ __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& 
   }
 }
 
-// Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.
-template <int D, int ROWS, bool GLOBAL, typename At>
+// Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.  A thread takes
+// ITEMS times four features side by side, and four parts at a time, so that their loads are under way together.
+template <int D, int ROWS, bool GLOBAL, int ITEMS, typename At>
 __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, int max_rows, int members, At at, float* dst, int tid, int nthr) {
-  const int rows = unit_rows<ROWS>(p, u.many, u.rt);
-  for (int e = tid; e < rows * (D / 4); e += nthr) {
-    const int row = e / (D / 4), f = (e - row * (D / 4)) * 4;
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < members; ++i) {
-      const float* s = at(i) + max_rows * D + row;
-      m = fmaxf(m, GLOBAL ? __ldcg(s) : *s);
+  const int items = unit_rows<ROWS>(p, u.many, u.rt) * (D / 4);
+  for (int e0 = tid; e0 < items; e0 += ITEMS * nthr) {
+    float m[ITEMS], l[ITEMS];
+    float4 x[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      m[k] = -INFINITY;
+      l[k] = 0.0f;
+      x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    const float base = m == -INFINITY ? 0.0f : m;
-    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int i = 0; i < members; ++i) {
-      const float* s = at(i);
-      const float* q = s + max_rows * D + row;
-      const float4 v = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(s + row * D + f)) : *reinterpret_cast<const float4*>(s + row * D + f);
-      const float w = ex2_approx((GLOBAL ? __ldcg(q) : *q) - base);
-      l += w * (GLOBAL ? __ldcg(q + max_rows) : q[max_rows]);
-      x.x += w * v.x; x.y += w * v.y; x.z += w * v.z; x.w += w * v.w;
-    }
-    if (dst) {
-      *reinterpret_cast<float4*>(dst + row * D + f) = x;
-      if (f == 0) {
-        dst[max_rows * D + row] = m;
-        dst[max_rows * (D + 1) + row] = l;
+    for (int i0 = 0; i0 < members; i0 += 4) {
+      float ms[ITEMS][4], ls[ITEMS][4];
+      float4 v[ITEMS][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* s = at(min(i0 + i, members - 1));
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+          const int e = min(e0 + k * nthr, items - 1), row = e / (D / 4), f = (e - row * (D / 4)) * 4;
+          const float* q = s + max_rows * D + row;
+          ms[k][i] = GLOBAL ? __ldcg(q) : *q;
+          ls[k][i] = GLOBAL ? __ldcg(q + max_rows) : q[max_rows];
+          v[k][i] = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(s + row * D + f)) : *reinterpret_cast<const float4*>(s + row * D + f);
+          if (i0 + i >= members) ms[k][i] = -INFINITY;
+        }
       }
-    } else {
-      write_row<ROWS>(p, u, row, f, x, m, l);
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const float top = fmaxf(m[k], fmaxf(fmaxf(ms[k][0], ms[k][1]), fmaxf(ms[k][2], ms[k][3]))), base = top == -INFINITY ? 0.0f : top;
+        const float c = ex2_approx(m[k] - base);
+        m[k] = top;
+        l[k] *= c;
+        x[k].x *= c; x[k].y *= c; x[k].z *= c; x[k].w *= c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i0 + i >= members) continue;
+          const float w = ex2_approx(ms[k][i] - base);
+          l[k] += w * ls[k][i];
+          x[k].x += w * v[k][i].x; x[k].y += w * v[k][i].y; x[k].z += w * v[k][i].z; x[k].w += w * v[k][i].w;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const int e = e0 + k * nthr, row = e / (D / 4), f = (e - row * (D / 4)) * 4;
+      if (e >= items) continue;
+      if (dst) {
+        *reinterpret_cast<float4*>(dst + row * D + f) = x[k];
+        if (f == 0) {
+          dst[max_rows * D + row] = m[k];
+          dst[max_rows * (D + 1) + row] = l[k];
+        }
+      } else {
+        write_row<ROWS>(p, u, row, f, x[k], m[k], l[k]);
+      }
     }
   }
 }

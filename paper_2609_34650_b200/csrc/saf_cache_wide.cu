@@ -6,18 +6,17 @@
 // the tensor core about 1000 clk, whatever the rows, of the 2800 that DRAM needs for its 64 KB (head dimension 128).  Two blocks an SM, so that one's
 // chain of scores, softmax and second product runs while the other's waits.
 //
-// Per block (384 threads): warps 0-7 compute, warps 8-10 fetch pages by TMA (a thread issues a copy in about 300 clk, and pages of 16
-// tokens take 24 copies a tile), warp 11 issues the MMAs and owns TMEM.  Two compute threads
-// share a row (= TMEM lane), each with 64 keys of a tile; TMEM columns [0,128) S (fp32), then weights (bf16 pairs in [0,32) and
-// [64,96)), [128,256) O.  Frozen rows replace their scores by alpha + rho out of a band that is copied in one tile ahead: 128
-// preferences of keys and 256 of distances for each of up to FZ frozen heads; other tiles (those that hold new tokens, more
-// frozen heads, positions far apart) take them from global memory in a pass of their own.
+// Per block (192 threads): warps 0-3 compute, a thread a row (= TMEM lane) with its 128 scores in registers (two threads a row spilled
+// 700 bytes at the 96 registers that twice the threads leave, and took 10000 clk a tile), warp 4 fetches pages by TMA, warp 5 issues the
+// MMAs and owns TMEM.  TMEM columns [0,128) S (fp32), then weights (bf16 pairs) in [0,64), [128,256) O.  Frozen rows replace their
+// scores by alpha + rho out of a band that is copied in one tile ahead: 128 preferences of keys and 256 of distances for each of
+// up to FZ frozen heads; with more of them, or positions far apart, they take them from global memory.
 #include "saf_cache_attn.cuh"
 
 namespace saf {
 namespace {
 
-constexpr int ROWS = 128, KT = 128, PRODUCERS = 1, W = 9 + PRODUCERS, NT = 32 * W, FZ = 4;
+constexpr int ROWS = 128, KT = 128, W = 6, NT = 32 * W, FZ = 4;
 constexpr int SINGLE_TILES = 8;     // tiles up to which a block takes a whole unit where there are no more units than blocks
 constexpr int BLOCKS = 2;           // blocks an SM
 
@@ -28,11 +27,9 @@ struct Cfg {
   static constexpr int TILE = PANELS * PANEL;
   static constexpr int ST = D == 64 ? 2 : 1;                 // tiles of keys, and of values, in shared memory
   static constexpr int OFF_Q = 0, OFF_K = TILE, OFF_V = OFF_K + ST * TILE, OFF_TAB = OFF_V + ST * TILE;
-  // words: bands [2][FZ][384], row maxima (at the end sums) [2][128], rows' masks [128] (two words), rows and heads [2][128],
-  // positions of new tokens [64], frozen heads [FZ]
-  static constexpr int TAB = 2 * FZ * 384 + 256 + 256 + 256 + 64 + FZ;
+  // words: bands [2][FZ][384], positions of new tokens [64], frozen heads [FZ]
+  static constexpr int TAB = 2 * FZ * 384 + 64 + FZ;
   static constexpr int SMEM = OFF_TAB + TAB * 4 + 1024;
-  static constexpr int HALF = D == 64 ? 32 : 64;             // output features of a compute thread
 };
 
 enum WideSite { SITE_K_EMPTY = 111, SITE_V_EMPTY, SITE_Q_FULL, SITE_K_FULL, SITE_P_FULL, SITE_V_FULL, SITE_O_FREE, SITE_S_FULL, SITE_PV_DONE };
@@ -48,20 +45,11 @@ __device__ __forceinline__ float ld_shared_f(uint32_t addr) {
 }
 __device__ __forceinline__ bool wild16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
-// Smallest position of a unit's tokens.
-__device__ __forceinline__ int band_pmin(const int* newpos, int first, int tokens) {
-  int lo = 0x7fffffff;
-  for (int c = threadIdx.x & 31; c < tokens; c += 32) lo = min(lo, newpos[first + c]);
-  return __reduce_min_sync(0xffffffffu, lo);
-}
-
-// Scores of frozen rows without a band, from global memory: written over what the score MMA left, half a row a thread.
-template <int D>
-__device__ __noinline__ void slow_scores(const CacheAttnParams& p, const Unit& w, int ctx, int t, int hh, int rowl, bool keys, bool frozen, uint32_t t_s,
-                                         const int* newpos, const int* row_h, const int* row_n) {
-  const int64_t head = static_cast<int64_t>(row_h[rowl]) * p.Tp;
-  const int pos = newpos[row_n[rowl] - w.first];
-  for (int cc = 0; cc < 4; ++cc) {
+// Scores of frozen rows without a band, from global memory: written over what the score MMA left.
+__device__ __noinline__ void slow_scores(const CacheAttnParams& p, const Unit& w, int ctx, int t, int h, int pos, bool keys, bool frozen, uint32_t t_s,
+                                         const int* newpos) {
+  const int64_t head = static_cast<int64_t>(h) * p.Tp;
+  for (int cc = 0; cc < 8; ++cc) {
     uint32_t r[16];
     if (keys) {
       tmem_ld16(t_s + 16 * cc, r);
@@ -69,11 +57,11 @@ __device__ __noinline__ void slow_scores(const CacheAttnParams& p, const Unit& w
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int j = t * KT + 64 * hh + 16 * cc + e, back = j - ctx;
+      const int j = t * KT + 16 * cc + e, back = j - ctx;
       float x = keys ? __uint_as_float(r[e]) : 0.0f;
       if (frozen) {
         const int pj = back < 0 ? j : j < w.len ? newpos[back] : 0x7fffffff;
-        x = pj <= pos ? (p.alpha[head + pj] + p.rho[head + pos - pj]) * LOG2E : -INFINITY;
+        x = pj <= pos ? p.alpha[head + pj] + p.rho[head + pos - pj] : -INFINITY;
       }
       r[e] = __float_as_uint(x);
     }
@@ -88,7 +76,7 @@ template <int D>
 __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint32_t vs, int tid) {
   constexpr int PANELS = Cfg<D>::PANELS;
   bool wild = false;
-  for (int c = tid; c < Cfg<D>::TILE / 16; c += 256) {
+  for (int c = tid; c < Cfg<D>::TILE / 16; c += 128) {
     const int box = c / (8 * br * PANELS), j = j0 + box * br + ((c >> 3) & (br - 1));
     if (j < ctx) continue;
     const uint32_t addr = vs + c * 16;
@@ -122,11 +110,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s, frozen_s;
   __shared__ uint32_t tmem_slot;
   float* bands = reinterpret_cast<float*>(smem + C::OFF_TAB);
-  float* xch = bands + 2 * FZ * 384;
-  unsigned long long* row_mask = reinterpret_cast<unsigned long long*>(xch + 256);
-  int* row_n = reinterpret_cast<int*>(row_mask + 128);
-  int* row_h = row_n + 128;
-  int* newpos = row_h + 128;
+  int* newpos = reinterpret_cast<int*>(bands + 2 * FZ * 384);
   int* fheads = newpos + 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const WaitCtx wc{&abort_s, p.status, p.wait_limit_ns};
@@ -134,16 +118,16 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     abort_s = 0;
     open_unit[0].start = open_unit[1].start = -1;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], PRODUCERS);
+      mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], 1);
-      mbar_init(&v_full[s], PRODUCERS);
+      mbar_init(&v_full[s], 1);
       mbar_init(&v_empty[s], 1);
     }
-    mbar_init(&q_full, 8);                                   // (one arrival per compute warp)
+    mbar_init(&q_full, 4);                                   // (one arrival per compute warp)
     mbar_init(&s_full, 1);
-    mbar_init(&p_full, 8);
+    mbar_init(&p_full, 4);
     mbar_init(&pv_done, 1);
-    mbar_init(&o_free, 8);
+    mbar_init(&o_free, 4);
     mbar_fence_init();
     tma_prefetch_desc(&mk);
     tma_prefetch_desc(&mv);
@@ -176,11 +160,11 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   const int g = p.kv_group;
 
   if (x0 >= x1) {
-  } else if (warp >= 8 && warp < W - 1) {
-    // ---------------------------------------------------------------- pages: every third copy of a tile
+  } else if (warp == W - 2) {
+    // ---------------------------------------------------------------- pages
     uint32_t nk = 0, nv = 0;
     bool ok = true;
-    const int br = p.box_rows, me = warp - 8;
+    const int br = p.box_rows;
     constexpr int VB = D == 128 ? 1 : C::PANELS;             // copies of a box of values (128: both halves at once)
     for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
       const int tb = tile_at(u, x0), te = tile_at(u, x1);
@@ -202,10 +186,10 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           ok = mbar_wait_warp_compact(half ? &v_empty[s] : &k_empty[s], ((n / C::ST) & 1) ^ 1, wc, half ? SITE_V_EMPTY : SITE_K_EMPTY);
           if (!ok) break;
           ++n;
-          const int split = half ? VB : C::PANELS, copies = boxes * split, mine = copies > me ? (copies - me + PRODUCERS - 1) / PRODUCERS : 0;
-          if (lane == 0) mbar_expect_tx(full, mine * br * 128 * (C::PANELS / split));
+          const int split = half ? VB : C::PANELS;
+          if (lane == 0) mbar_expect_tx(full, boxes * br * 128 * C::PANELS);
           uint8_t* dst = smem + (half ? C::OFF_V : C::OFF_K) + s * C::TILE;
-          for (int x = me; x < copies; x += PRODUCERS) {
+          for (int x = 0; x < boxes * split; ++x) {
             const int c = split == 2 ? x >> 1 : x, pn = split == 2 ? x & 1 : 0;
             const int page = __shfl_sync(0xffffffffu, ids, (t - ids_at) * 8 + c * (br >> 4)), at = t * KT + c * br;
             const int slot = p.page_shift >= 0 ? at & (p.page_size - 1) : at % p.page_size;
@@ -268,8 +252,8 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         tc_fence_after();
         if (leader) {
 #pragma unroll
-          for (int kc = 0; kc < 8; ++kc)                      // (bf16 pairs: keys 0-63 in columns [0,32), keys 64-127 in [64,96))
-            umma_ts2(tmem + 128, tmem + 8 * kc + (kc >= 4 ? 32u : 0u),
+          for (int kc = 0; kc < 8; ++kc)
+            umma_ts2(tmem + 128, tmem + 8 * kc,
                      lo_m + ((C::OFF_V + s * C::TILE + ((kc * 16 / br) * C::PANELS * br + kc * 16 % br) * 128) >> 4), hi_m, idesc_o, kc > 0 || t > tb ? 1u : 0u);
           umma_commit(&v_empty[s]);
           umma_commit(&pv_done);
@@ -280,13 +264,10 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     }
   } else {
     // ---------------------------------------------------------------- softmax
-    // (what is not needed in the loop over tiles lies in shared memory: the 64 scores of a thread leave few registers)
-    const int hh = warp >> 2, rowl = (warp & 3) * 32 + lane;
-    const uint32_t t_s = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 64 * hh;
-    const uint32_t t_o = t_s + 128 - 64 * hh + C::HALF * hh;
+    const uint32_t t_s = tmem + (static_cast<uint32_t>(warp * 32) << 16);
     uint32_t count = 0;                                      // tiles so far
     bool ok = true;
-    // (a warp whose wait was abandoned walks on, without storing, until all eight leave together)
+    // (a warp whose wait was abandoned walks on, without storing, until all four leave together)
     for (uint32_t k = 0;; ++k) {
       if (tid == 0) {
         Unit v = work[(k & 1) ^ 1];
@@ -297,166 +278,153 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         range_s[k & 1][0] = more ? tile_at(v, x0) : 0;
         range_s[k & 1][1] = more ? tile_at(v, x1) : -1;
       }
-      if (named_bar_or(5, 256, !ok)) break;
+      if (named_bar_or(5, 128, !ok)) break;
       const int tb = range_s[k & 1][0], te = range_s[k & 1][1];
       if (te < 0) break;
       const Unit& w = work[k & 1];
       const int ctx = w.len - w.many, rows = unit_rows<ROWS>(p, w.many, w.rt);
-      const bool keys = has_keys(p, w.hk), there = rowl < rows;
-      const bool idle = (warp & 3) * 32 >= rows;             // none of the warp's rows is there
-      bool frozen = false, any_frozen = false, fast = false;
-      uint32_t band_at = 0;                                  // this row's place in the band: alpha of key 0 of its half
+      const bool keys = has_keys(p, w.hk), there = tid < rows, idle = warp * 32 >= rows;
+      int i, hg;
+      row_at<ROWS>(p, w.many, w.rt, there ? tid : 0, i, hg);
+      const int h = w.hk * g + hg, n = w.first + i;
+      const bool frozen = (p.frozen[h >> 5] >> (h & 31)) & 1;
+      unsigned long long mask = !there ? 0 : p.masks ? p.masks[n] : (2ull << i) - 1;
+      if (w.many < 64) mask &= (1ull << w.many) - 1;
+      if (keys) {
+        // queries of ordinary rows, zeros elsewhere, as the swizzled tile that TMA would leave
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(n) * p.q_strides[0] + h * p.q_strides[1];
+        const uint32_t base = smem_u32(smem) + C::OFF_Q + tid * 128;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          const uint4 x = there && !frozen ? *reinterpret_cast<const uint4*>(q + c * 8) : make_uint4(0, 0, 0, 0);
+          st_shared_v4w(base + (c >> 3) * C::PANEL + (((c & 7) ^ (tid & 7)) << 4), x.x, x.y, x.z, x.w);
+        }
+        fence_proxy_async_smem();
+        warp_arrive(&q_full);
+      }
+      // frozen heads of the group, positions of the new tokens
+      if (tid == 0) {
+        int found = 0;
+        for (int c = 0; c < g; ++c) {
+          const int hk = w.hk * g + c;
+          if ((p.frozen[hk >> 5] >> (hk & 31)) & 1) {
+            if (found < FZ) fheads[found] = hk;
+            ++found;
+          }
+        }
+        frozen_s = found;
+        wild_s = 0;
+      }
+      if (tid < w.many) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
+      named_bar_sync(6, 128);
+      const int n_frozen = frozen_s;
+      bool any_frozen = false, fast = false;
+      uint32_t band_at = 0;                                  // this row's band: alpha of key 0
       int rho_at = 0;                                        // from there to rho of that key
-      {
-        int i, hg;
-        row_at<ROWS>(p, w.many, w.rt, there ? rowl : 0, i, hg);
-        const int h = w.hk * g + hg, n = w.first + i;
-        frozen = (p.frozen[h >> 5] >> (h & 31)) & 1;
-        unsigned long long mask = !there ? 0 : p.masks ? p.masks[n] : (2ull << i) - 1;
-        if (w.many < 64) mask &= (1ull << w.many) - 1;
-        if (keys) {
-          // queries of ordinary rows, zeros elsewhere, as the swizzled tile that TMA would leave
-          const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(n) * p.q_strides[0] + h * p.q_strides[1];
-          constexpr int CH = D == 64 ? 4 : 8;
-          uint4 x[CH];
-#pragma unroll
-          for (int c = 0; c < CH; ++c) {
-            const int f = (hh * CH + c) * 8;
-            x[c] = there && !frozen && f < D ? *reinterpret_cast<const uint4*>(q + f) : make_uint4(0, 0, 0, 0);
-          }
-          const uint32_t base = smem_u32(smem) + C::OFF_Q + (D == 64 ? 0 : hh * C::PANEL) + rowl * 128;
-#pragma unroll
-          for (int c = 0; c < CH; ++c) st_shared_v4w(base + ((((D == 64 ? hh * CH : 0) + c) ^ (rowl & 7)) << 4), x[c].x, x[c].y, x[c].z, x[c].w);
-          fence_proxy_async_smem();
-          warp_arrive(&q_full);
+      int pos = 0, pmin = 0;
+      if (n_frozen > 0) {
+        pos = newpos[i];
+        int lo = 0x7fffffff, hi = 0;
+        for (int c = lane; c < rows / g; c += 32) {
+          const int x = newpos[w.rt * p.tile_tokens + c];
+          lo = min(lo, x);
+          hi = max(hi, x);
         }
-        // frozen heads of the group, positions of the new tokens
-        if (tid == 0) {
-          int found = 0;
-          for (int c = 0; c < g; ++c) {
-            const int hk = w.hk * g + c;
-            if ((p.frozen[hk >> 5] >> (hk & 31)) & 1) {
-              if (found < FZ) fheads[found] = hk;
-              ++found;
-            }
-          }
-          frozen_s = found;
-          wild_s = 0;
+        pmin = __reduce_min_sync(0xffffffffu, lo);
+        const int span = __reduce_max_sync(0xffffffffu, hi) - pmin;
+        fast = n_frozen <= FZ && pmin >= ctx && span < 64 && ctx >= 0;
+        if (frozen && p.positions) {                         // (new tokens behind the row's position are not seen)
+          for (int c = 0; c < w.many; ++c)
+            if (newpos[c] > pos) mask &= ~(1ull << c);
         }
-        if (tid < w.many) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
-        named_bar_sync(6, 256);
-        const int n_frozen = frozen_s;
-        if (n_frozen > 0) {
-          const int pos = newpos[i], tokens = rows / g;
-          int lo = 0x7fffffff, hi = 0;
-          for (int c = lane; c < tokens; c += 32) {
-            const int x = newpos[w.rt * p.tile_tokens + c];
-            lo = min(lo, x);
-            hi = max(hi, x);
-          }
-          const int pmin = __reduce_min_sync(0xffffffffu, lo), span = __reduce_max_sync(0xffffffffu, hi) - pmin;
-          fast = n_frozen <= FZ && pmin >= ctx && span < 64 && ctx >= 0;
-          if (frozen && p.positions) {                       // (new tokens behind the row's position are not seen)
-            for (int c = 0; c < w.many; ++c)
-              if (newpos[c] > pos) mask &= ~(1ull << c);
-          }
-          int slot = 0;
-          for (int c = 0; c < min(n_frozen, FZ); ++c)
-            if (fheads[c] == h) slot = c;
-          band_at = smem_u32(bands + slot * 384 + 64 * hh);
-          rho_at = (128 - 64 * hh + min(max(pos - pmin, 0), 63) + 127 - 64 * hh) * 4;
-          any_frozen = __any_sync(0xffffffffu, frozen && there);
-        }
-        row_mask[rowl] = mask;
-        row_n[rowl] = n;
-        row_h[rowl] = h;
+        int slot = 0;
+        for (int c = 0; c < min(n_frozen, FZ); ++c)
+          if (fheads[c] == h) slot = c;
+        band_at = smem_u32(bands + slot * 384);
+        rho_at = (128 + min(max(pos - pmin, 0), 63) + 127) * 4;
+        any_frozen = __any_sync(0xffffffffu, frozen && there);
       }
       // A tile's band: alpha of its keys' positions, then rho of distances pmin - (j0 + 127) and up (what lies outside the vectors
       // belongs to keys that are not seen).
       auto fetch_band = [&](int t) {
-        const int j0 = t * KT, n_frozen = frozen_s, pmin = w.many > 0 ? band_pmin(newpos, w.rt * p.tile_tokens, rows / g) : 0;
-        for (int x = tid; x < n_frozen * 384; x += 256) {
-          const int s = x / 384, y = x - s * 384;
-          const int64_t head = static_cast<int64_t>(fheads[s]) * p.Tp;
-          const int j = j0 + y, at = y < 128 ? (j < ctx ? j : j < w.len ? newpos[j - ctx] : -1) : pmin - j0 - 127 + (y - 128);
-          const bool in = at >= 0 && at < p.Tp;
-          copy4(smem_u32(bands + ((t & 1) * FZ + s) * 384 + y), (y < 128 ? p.alpha : p.rho) + head + (in ? at : 0), in);
+        const int j = t * KT + tid, at = j < ctx ? j : j < w.len ? newpos[j - ctx] : -1, d = pmin - t * KT - 127 + tid;
+        uint32_t dst = smem_u32(bands + (t & 1) * FZ * 384 + tid);
+        for (int c = 0; c < n_frozen; ++c, dst += 384 * 4) {
+          const int64_t head = static_cast<int64_t>(fheads[c]) * p.Tp;
+          copy4(dst, p.alpha + head + max(at, 0), at >= 0);
+          const bool in0 = d >= 0 && d < p.Tp, in1 = d + 128 >= 0 && d + 128 < p.Tp;
+          copy4(dst + 128 * 4, p.rho + head + (in0 ? d : 0), in0);
+          copy4(dst + 256 * 4, p.rho + head + (in1 ? d + 128 : 0), in1);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
       if (fast) fetch_band(tb);
-      const float cf = frozen ? 1.0f : p.scale_log2;          // (frozen scores are formed in powers of two)
+      const float cf = frozen ? LOG2E : p.scale_log2;         // from scores to powers of two
       float m_ref = -INFINITY, l = 0.0f;
       for (int t = tb; t < te; ++t, ++count) {
         const bool plain = (t + 1) * KT <= ctx;               // all of its keys were cached before the step
         if (fast) {
           asm volatile("cp.async.wait_all;" ::: "memory");
-          named_bar_sync(6, 256);                             // (the band of this tile is there, that of the one before has been read)
+          named_bar_sync(6, 128);                             // (the band of this tile is there, that of the one before has been read)
           if (t + 1 < te) fetch_band(t + 1);
         }
         if (!mbar_wait_warp_compact(&s_full, count & 1, wc, SITE_S_FULL)) ok = false;
         if (t > tb && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
         tc_fence_after();
         if (!idle) {
-          if (any_frozen && !fast) slow_scores<D>(p, w, ctx, t, hh, rowl, keys, frozen, t_s, newpos, row_h, row_n);
-          uint32_t r0[32], r1[32];
-          if (keys || !fast) {
-            tmem_ld32(t_s, r0);
-            tmem_ld32(t_s + 32, r1);
-            tmem_wait_ld();
-          }
-          if (any_frozen && fast) {
-            const uint32_t a = band_at + (t & 1) * (FZ * 384 * 4);
-            if (plain) {
+          if (any_frozen && !fast) slow_scores(p, w, ctx, t, h, pos, keys, frozen, t_s, newpos);
+          // 32 scores at a time, so that loads have registers to arrive in: first the maximum (what differs from the MMA's scores is
+          // written back), then the weights
+          const bool written = (any_frozen && fast) || !plain;
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {                       // (not unrolled: the loop over tiles has to stay in the instruction cache)
+            uint32_t r[32];
+            if (keys || !fast) {
+              tmem_ld32(t_s + 32 * c, r);
+              tmem_wait_ld();
+            }
+            if (any_frozen && fast) {
+              const uint32_t a = band_at + (t & 1) * (FZ * 384 * 4) + 128 * c;
+              if (plain) {
+                float x[32], y[32];
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                float a0[4], a1[4];
-                ld_shared_v4f(a + 4 * e, a0[0], a0[1], a0[2], a0[3]);
-                ld_shared_v4f(a + 4 * (32 + e), a1[0], a1[1], a1[2], a1[3]);
+                for (int e = 0; e < 32; e += 4) ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  const float s0 = (a0[c] + ld_shared_f(a + rho_at - 4 * (e + c))) * LOG2E;
-                  const float s1 = (a1[c] + ld_shared_f(a + rho_at - 4 * (32 + e + c))) * LOG2E;
-                  if (frozen) {
-                    r0[e + c] = __float_as_uint(s0);
-                    r1[e + c] = __float_as_uint(s1);
-                  }
+                for (int e = 0; e < 32; ++e) y[e] = ld_shared_f(a + rho_at - 256 * c - 4 * e);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
+              } else {
+                // keys of new tokens lie at their positions
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  const int back = t * KT + 32 * c + e - ctx, at = back < 0 || back >= w.many ? 32 * c + e : newpos[back] - t * KT;
+                  const float y = ld_shared_f(a + 4 * e) + ld_shared_f(a - 128 * c + rho_at - 4 * min(at, 127));
+                  if (frozen) r[e] = __float_as_uint(y);
                 }
               }
-            } else {
-              // keys of new tokens lie at their positions
-              const int j = t * KT + 64 * hh;
-#pragma unroll
-              for (int e = 0; e < 64; ++e) {
-                const int back = j + e - ctx, at = back < 0 || back >= w.many ? e : newpos[back] - j;
-                const float x = (ld_shared_f(a + 4 * e) + ld_shared_f(a + rho_at - 4 * min(at, 127 - 64 * hh))) * LOG2E;
-                if (frozen) (e < 32 ? r0[e & 31] : r1[e & 31]) = __float_as_uint(x);
-              }
             }
-          }
-          if (!plain) {
-            // which of the thread's 64 keys the row sees
-            const int rel = ctx - (t * KT + 64 * hh);
-            const unsigned long long m = row_mask[rowl];
-            const unsigned long long sees = rel >= 64 ? ~0ull : rel > 0 ? ((1ull << rel) - 1) | (m << rel) : rel > -64 ? m >> -rel : 0ull;
+            if (!plain) {
+              // which keys the row sees
+              const int rel = ctx - (t * KT + 32 * c);
+              const uint32_t sees = rel >= 32 ? ~0u : rel > 0 ? ((1u << rel) - 1) | (static_cast<uint32_t>(mask) << rel) : rel > -64 ? static_cast<uint32_t>(mask >> -rel) : 0u;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              if (!((static_cast<uint32_t>(sees) >> e) & 1)) r0[e] = 0xff800000u;
-              if (!((static_cast<uint32_t>(sees >> 32) >> e) & 1)) r1[e] = 0xff800000u;
+              for (int e = 0; e < 32; ++e)
+                if (!((sees >> e) & 1)) r[e] = 0xff800000u;
             }
-          }
-          float mx0 = -INFINITY, mx1 = -INFINITY;
+            if (written) tmem_st32(t_s + 32 * c, r);
+            float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            mx0 = max3(mx0, __uint_as_float(r0[e]), __uint_as_float(r0[e + 1]));
-            mx1 = max3(mx1, __uint_as_float(r1[e]), __uint_as_float(r1[e + 1]));
+            for (int e = 0; e < 32; e += 4) {
+              mx0 = max3(mx0, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+              mx1 = max3(mx1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+            }
+            top = max3(top, mx0, mx1);
           }
-          float mx = fmaxf(mx0, mx1);
-          xch[hh * 128 + rowl] = mx;
-          named_bar_sync(1 + (warp & 3), 64);
-          mx = fmaxf(mx, xch[(hh ^ 1) * 128 + rowl]);
+          if (written) tmem_wait_st();
           // the reference follows the maximum where that has grown by more than 2^8
-          const float m_new = fmaxf(m_ref, mx * cf);
+          const float m_new = fmaxf(m_ref, top * cf);
           const bool need = m_new - m_ref > 8.0f;             // (from -inf: always; -inf to -inf: NaN, no)
           if (t == tb) {
             m_ref = m_new;
@@ -465,38 +433,32 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             l *= f;
             if (need) m_ref = m_new;
 #pragma unroll 1
-            for (int cc = 0; cc < C::HALF / 16; ++cc) {
-              uint32_t r[16];
-              tmem_ld16(t_o + 16 * cc, r);
+            for (int cc = 0; cc < D / 16; ++cc) {
+              uint32_t x[16];
+              tmem_ld16(t_s + 128 + 16 * cc, x);
               tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-              tmem_st16(t_o + 16 * cc, r);
+              for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+              tmem_st16(t_s + 128 + 16 * cc, x);
             }
           }
           const float neg_m = m_ref == -INFINITY ? 0.0f : -m_ref;
-          float l0 = 0.0f, l1 = 0.0f;
-          {
-            uint32_t pk[16];
+          float sum[2] = {0.0f, 0.0f};
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {                       // (the weights of 32 keys take the place of scores that have been read)
+            uint32_t r[32], pk[16];
+            tmem_ld32(t_s + 32 * c, r);
+            tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float a0 = ex2_approx(fmaf(__uint_as_float(r0[2 * e]), cf, neg_m)), a1 = ex2_approx(fmaf(__uint_as_float(r0[2 * e + 1]), cf, neg_m));
-              l0 += a0 + a1;
+              const float a0 = ex2_approx(fmaf(__uint_as_float(r[2 * e]), cf, neg_m)), a1 = ex2_approx(fmaf(__uint_as_float(r[2 * e + 1]), cf, neg_m));
+              sum[0] += a0;
+              sum[1] += a1;
               pk[e] = pack_bf16x2(a0, a1);
             }
-            tmem_st16(t_s, pk);
+            tmem_st16(t_s + 16 * c, pk);
           }
-          {
-            uint32_t pk[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float a0 = ex2_approx(fmaf(__uint_as_float(r1[2 * e]), cf, neg_m)), a1 = ex2_approx(fmaf(__uint_as_float(r1[2 * e + 1]), cf, neg_m));
-              l1 += a0 + a1;
-              pk[e] = pack_bf16x2(a0, a1);
-            }
-            tmem_st16(t_s + 16, pk);
-          }
-          l += l0 + l1;
+          l += sum[0] + sum[1];
         }
         if (!plain) {
           if (!mbar_wait_warp_compact(&v_full[count % C::ST], (count / C::ST) & 1, wc, SITE_V_FULL)) ok = false;
@@ -507,59 +469,54 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         tc_fence_before();
         warp_arrive(&p_full);
       }
-      named_bar_sync(6, 256);                                 // (the last maxima have been read)
-      xch[hh * 128 + rowl] = l;
-      named_bar_sync(1 + (warp & 3), 64);
-      l += xch[(hh ^ 1) * 128 + rowl];
-      if (!mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
+      if (!mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;   // (behind it all four warps have set wild_s)
       tc_fence_after();
       const bool whole = tb == 0 && te == w.tiles;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // (NaN stays NaN)
-      const int n = row_n[rowl], h = row_h[rowl];
       float* part = slot_of(blockIdx.x, w.start);
+      if (!idle) {
+#pragma unroll 1
+        for (int f0 = 0; f0 < D; f0 += 32) {
+          uint32_t r[32];
+          __syncwarp();
+          tmem_ld32(t_s + 128 + f0, r);
+          tmem_wait_ld();
+          if (wild_s && there) {
+            for (int back = max(tb * KT - ctx, 0); back < w.many && ctx + back < min(te * KT, w.len); ++back) {
+              const int j = ctx + back;
+              if (j < 0 || !((mask >> back) & 1)) continue;
+              const int page = min(max(p.block_table[static_cast<int64_t>(w.r) * p.max_pages + j / p.page_size], 0), p.n_pages - 1);
+              const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + page * p.v_strides[0] + w.hk * p.v_strides[1] + (j % p.page_size) * p.v_strides[2] + f0;
 #pragma unroll
-      for (int cc = 0; cc < C::HALF / 32; ++cc) {
-        const int f0 = C::HALF * hh + 32 * cc;
-        if (f0 >= D) break;
-        uint32_t r[32];
-        __syncwarp();
-        tmem_ld32(t_o + 32 * cc, r);
-        tmem_wait_ld();
-        if (wild_s && there) {
-          for (int back = max(tb * KT - ctx, 0); back < w.many && ctx + back < min(te * KT, w.len); ++back) {
-            const int j = ctx + back;
-            if (j < 0 || !((row_mask[rowl] >> back) & 1)) continue;
-            const int page = min(max(p.block_table[static_cast<int64_t>(w.r) * p.max_pages + j / p.page_size], 0), p.n_pages - 1);
-            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + page * p.v_strides[0] + w.hk * p.v_strides[1] + (j % p.page_size) * p.v_strides[2] + f0;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float x = __bfloat162float(v[e]);
-              if (!isfinite(x)) r[e] = __float_as_uint(__uint_as_float(r[e]) + x);
+              for (int e = 0; e < 32; ++e) {
+                const float x = __bfloat162float(v[e]);
+                if (!isfinite(x)) r[e] = __float_as_uint(__uint_as_float(r[e]) + x);
+              }
             }
           }
-        }
-        if (there && ok && whole) {
-          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.O) + static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + f0;
+          if (there && ok && whole) {
+            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.O) + static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + f0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint4 x;
-            x.x = pack_bf16x2(__uint_as_float(r[8 * c]) * inv, __uint_as_float(r[8 * c + 1]) * inv);
-            x.y = pack_bf16x2(__uint_as_float(r[8 * c + 2]) * inv, __uint_as_float(r[8 * c + 3]) * inv);
-            x.z = pack_bf16x2(__uint_as_float(r[8 * c + 4]) * inv, __uint_as_float(r[8 * c + 5]) * inv);
-            x.w = pack_bf16x2(__uint_as_float(r[8 * c + 6]) * inv, __uint_as_float(r[8 * c + 7]) * inv);
-            *reinterpret_cast<uint4*>(o + 8 * c) = x;
+            for (int c = 0; c < 4; ++c) {
+              uint4 x;
+              x.x = pack_bf16x2(__uint_as_float(r[8 * c]) * inv, __uint_as_float(r[8 * c + 1]) * inv);
+              x.y = pack_bf16x2(__uint_as_float(r[8 * c + 2]) * inv, __uint_as_float(r[8 * c + 3]) * inv);
+              x.z = pack_bf16x2(__uint_as_float(r[8 * c + 4]) * inv, __uint_as_float(r[8 * c + 5]) * inv);
+              x.w = pack_bf16x2(__uint_as_float(r[8 * c + 6]) * inv, __uint_as_float(r[8 * c + 7]) * inv);
+              *reinterpret_cast<uint4*>(o + 8 * c) = x;
+            }
+          } else if (there && ok) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              *reinterpret_cast<float4*>(part + tid * D + f0 + 4 * c) =
+                  make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]), __uint_as_float(r[4 * c + 3]));
           }
-        } else if (there && ok) {
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            *reinterpret_cast<float4*>(part + rowl * D + f0 + 4 * c) =
-                make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]), __uint_as_float(r[4 * c + 3]));
         }
       }
-      if (hh == 0 && there && ok) {
+      if (there && ok) {
         if (!whole) {
-          part[p.max_rows * D + rowl] = m_ref;
-          part[p.max_rows * (D + 1) + rowl] = l;
+          part[p.max_rows * D + tid] = m_ref;
+          part[p.max_rows * (D + 1) + tid] = l;
         } else if (p.LSE) {
           p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : (m_ref + log2f(l)) * LN2;
         }
@@ -594,7 +551,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     const Part unit = open_unit[k];
     if (unit.start < 0 || !arrived_s[k]) continue;
     const int first = cut_s.run_of(unit.start), last = cut_s.run_of(unit.last);
-    join<D, ROWS, true>(p, unit, p.max_rows, last - first + 1, [&](int i) { return slot_of(first + i, unit.start); }, nullptr, tid, NT);
+    join<D, ROWS, true, 4>(p, unit, p.max_rows, last - first + 1, [&](int i) { return slot_of(first + i, unit.start); }, nullptr, tid, NT);
   }
 }
 
