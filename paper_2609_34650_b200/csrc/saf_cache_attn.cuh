@@ -34,10 +34,15 @@ template <int KT, int ROWS>
 __device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) {
   set_request<KT, ROWS>(p, u, p.new_offsets[u.r], p.new_offsets[u.r + 1], p.kv_lens[u.r]);
 }
+// Places on the line that a unit takes behind its tiles, for what it costs besides: 128-row units begin and end slowly, and their last
+// tiles, with masks, take two to three times the others' time (24 trees of up to 32 tokens on contexts of up to 8192: the slowest block took
+// 1.8 times the mean without).
+template <int ROWS>
+constexpr int EXTRA = ROWS > 16 ? 3 : 0;
 // The next unit that has rows; u.r = p.R behind the last.
 template <int KT, int ROWS>
 __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {
-  u.start += u.pitch ? u.pitch : u.tiles;
+  u.start += u.pitch ? u.pitch : u.tiles + EXTRA<ROWS>;
   if (++u.rt < u.row_tiles) return;
   u.rt = 0;
   if (++u.hk >= p.heads_cached) {
@@ -193,7 +198,7 @@ __device__ __forceinline__ void place_run(const CacheAttnParams& p, uint8_t* sme
       if (r == p.R - 1) firsts[p.R] = last;
       lens[r] = len;
       set_request<KT, ROWS>(p, u, first, last, len);
-      cost += u.row_tiles * Hk * u.tiles;
+      cost += u.row_tiles * Hk * (u.tiles + EXTRA<ROWS>);
       units += u.row_tiles * Hk;
       if (u.many > 0) longest = max(longest, u.tiles);
       sums[r] = cost;
@@ -266,7 +271,7 @@ __device__ __forceinline__ void place_run(const CacheAttnParams& p, uint8_t* sme
     u.r = lo;
     u.start = lo > base ? sum(lo - 1) : off;
     set_request<KT, ROWS>(p, u, firsts[lo], firsts[lo + 1], lens[lo]);
-    const int step = pitch ? pitch : u.tiles, at = (x0 - u.start) / step;   // number of the unit within its request
+    const int step = pitch ? pitch : u.tiles + EXTRA<ROWS>, at = (x0 - u.start) / step;   // number of the unit within its request
     u.hk = u.row_tiles == 1 ? at : at / u.row_tiles;
     u.rt = at - u.hk * u.row_tiles;
     u.start += at * step;

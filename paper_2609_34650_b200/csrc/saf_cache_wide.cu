@@ -27,8 +27,8 @@ struct Cfg {
   static constexpr int TILE = PANELS * PANEL;
   static constexpr int ST = D == 64 ? 2 : 1;                 // tiles of keys, and of values, in shared memory
   static constexpr int OFF_Q = 0, OFF_K = TILE, OFF_V = OFF_K + ST * TILE, OFF_TAB = OFF_V + ST * TILE;
-  // words: bands [2][FZ][384], positions of new tokens [64], frozen heads [FZ]
-  static constexpr int TAB = 2 * FZ * 384 + 64 + FZ;
+  // words: bands [2][FZ][384], keys' places in a band [2][128], positions of new tokens [64], frozen heads [FZ]
+  static constexpr int TAB = 2 * FZ * 384 + 256 + 64 + FZ;
   static constexpr int SMEM = OFF_TAB + TAB * 4 + 1024;
 };
 
@@ -110,7 +110,8 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s, frozen_s;
   __shared__ uint32_t tmem_slot;
   float* bands = reinterpret_cast<float*>(smem + C::OFF_TAB);
-  int* newpos = reinterpret_cast<int*>(bands + 2 * FZ * 384);
+  int* places = reinterpret_cast<int*>(bands + 2 * FZ * 384);
+  int* newpos = places + 256;
   int* fheads = newpos + 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const WaitCtx wc{&abort_s, p.status, p.wait_limit_ns};
@@ -294,11 +295,11 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         // queries of ordinary rows, zeros elsewhere, as the swizzled tile that TMA would leave
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(n) * p.q_strides[0] + h * p.q_strides[1];
         const uint32_t base = smem_u32(smem) + C::OFF_Q + tid * 128;
+        uint4 x[D / 8];
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 x = there && !frozen ? *reinterpret_cast<const uint4*>(q + c * 8) : make_uint4(0, 0, 0, 0);
-          st_shared_v4w(base + (c >> 3) * C::PANEL + (((c & 7) ^ (tid & 7)) << 4), x.x, x.y, x.z, x.w);
-        }
+        for (int c = 0; c < D / 8; ++c) x[c] = there && !frozen ? *reinterpret_cast<const uint4*>(q + c * 8) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) st_shared_v4w(base + (c >> 3) * C::PANEL + (((c & 7) ^ (tid & 7)) << 4), x[c].x, x[c].y, x[c].z, x[c].w);
         fence_proxy_async_smem();
         warp_arrive(&q_full);
       }
@@ -348,6 +349,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       // belongs to keys that are not seen).
       auto fetch_band = [&](int t) {
         const int j = t * KT + tid, at = j < ctx ? j : j < w.len ? newpos[j - ctx] : -1, d = pmin - t * KT - 127 + tid;
+        if (j - tid + KT > ctx) places[(t & 1) * 128 + tid] = 4 * min(max(at < 0 ? tid : at - t * KT, -63), 127);   // (new tokens lie at their positions)
         uint32_t dst = smem_u32(bands + (t & 1) * FZ * 384 + tid);
         for (int c = 0; c < n_frozen; ++c, dst += 384 * 4) {
           const int64_t head = static_cast<int64_t>(fheads[c]) * p.Tp;
@@ -396,13 +398,18 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
                 for (int e = 0; e < 32; ++e)
                   if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
               } else {
-                // keys of new tokens lie at their positions
+                float x[32], y[32];
+                const uint32_t pl = smem_u32(places + (t & 1) * 128 + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  const int back = t * KT + 32 * c + e - ctx, at = back < 0 || back >= w.many ? 32 * c + e : newpos[back] - t * KT;
-                  const float y = ld_shared_f(a + 4 * e) + ld_shared_f(a - 128 * c + rho_at - 4 * min(at, 127));
-                  if (frozen) r[e] = __float_as_uint(y);
+                for (int e = 0; e < 32; e += 4) {
+                  ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
+                  ld_shared_v4f(pl + 4 * e, y[e], y[e + 1], y[e + 2], y[e + 3]);
                 }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) y[e] = ld_shared_f(a - 128 * c + rho_at - __float_as_int(y[e]));
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
               }
             }
             if (!plain) {
