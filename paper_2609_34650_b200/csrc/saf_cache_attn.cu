@@ -545,7 +545,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     if (unit.start < 0) continue;
     const int w0 = unit.start <= b0 ? 0 : cut.run_of(unit.start) - run0;
     const int w1 = unit.last >= b1 ? W - 1 : cut.run_of(unit.last) - run0;
-    join<D, ROWS, false, 1>(p, unit, max_rows, w1 - w0 + 1, [&](int i) { return part_of(w0 + i, unit); }, slot_of(blockIdx.x, unit), threadIdx.x, NT);
+    join<D, ROWS, false, 1, 2>(p, unit, max_rows, w1 - w0 + 1, [&](int i) { return part_of(w0 + i, unit); }, slot_of(blockIdx.x, unit), threadIdx.x, NT);
   }
   const bool any_open = open_unit[0].start >= 0 || open_unit[1].start >= 0;
   int c_first = 0, c_last = 0;
@@ -565,7 +565,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   }
   if (lead.start >= 0) {
     const int members = cut.run_of(lead.last) - run0 - warp + 1;
-    join<D, ROWS, false, 1>(p, lead, max_rows, members, [&](int i) { return part_of(warp + i, lead); }, nullptr, lane, 32);
+    join<D, ROWS, false, 1, 2>(p, lead, max_rows, members, [&](int i) { return part_of(warp + i, lead); }, nullptr, lane, 32);
   }
   if (!any_open) return;
   __syncthreads();
@@ -574,7 +574,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     if (unit.start < 0 || !arrived_s[k]) continue;
     c_first = cut.run_of(unit.start) / W;
     c_last = cut.run_of(unit.last) / W;
-    join<D, ROWS, true, 1>(p, unit, max_rows, c_last - c_first + 1, [&](int i) { return slot_of(c_first + i, unit); }, nullptr, threadIdx.x, NT);
+    join<D, ROWS, true, 1, 4>(p, unit, max_rows, c_last - c_first + 1, [&](int i) { return slot_of(c_first + i, unit); }, nullptr, threadIdx.x, NT);
   }
 }
 

@@ -114,10 +114,12 @@ __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& 
 }
 
 // Joins `members` parts, in order, on `nthr` threads of which this is number `tid`: to the outputs, or (dst) to one part.  A thread takes
-// ITEMS times four features side by side, and four parts at a time, so that their loads are under way together.
-template <int D, int ROWS, bool GLOBAL, int ITEMS, typename At>
+// ITEMS times four features side by side, and AHEAD parts at a time, so that their loads are under way together; more than a few
+// of both is no faster, because this code is met cold and every instruction of it has to be fetched.
+template <int D, int ROWS, bool GLOBAL, int ITEMS, int AHEAD, typename At>
 __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, int max_rows, int members, At at, float* dst, int tid, int nthr) {
   const int items = unit_rows<ROWS>(p, u.many, u.rt) * (D / 4);
+#pragma unroll 1
   for (int e0 = tid; e0 < items; e0 += ITEMS * nthr) {
     float m[ITEMS], l[ITEMS];
     float4 x[ITEMS];
@@ -127,33 +129,40 @@ __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, in
       l[k] = 0.0f;
       x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    for (int i0 = 0; i0 < members; i0 += 4) {
-      float ms[ITEMS][4], ls[ITEMS][4];
-      float4 v[ITEMS][4];
+#pragma unroll 1
+    for (int i0 = 0; i0 < members; i0 += AHEAD) {
+      float ms[ITEMS][AHEAD], ls[ITEMS][AHEAD];
+      float4 v[ITEMS][AHEAD];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < AHEAD; ++i) {
         const float* s = at(min(i0 + i, members - 1));
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-          const int e = min(e0 + k * nthr, items - 1), row = e / (D / 4), f = (e - row * (D / 4)) * 4;
+          const int e = e0 + k * nthr, row = e / (D / 4), f = (e - row * (D / 4)) * 4;
           const float* q = s + max_rows * D + row;
-          ms[k][i] = GLOBAL ? __ldcg(q) : *q;
-          ls[k][i] = GLOBAL ? __ldcg(q + max_rows) : q[max_rows];
-          v[k][i] = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(s + row * D + f)) : *reinterpret_cast<const float4*>(s + row * D + f);
-          if (i0 + i >= members) ms[k][i] = -INFINITY;
+          ms[k][i] = -INFINITY;
+          ls[k][i] = 0.0f;
+          v[k][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (i0 + i < members && e < items) {
+            ms[k][i] = GLOBAL ? __ldcg(q) : *q;
+            ls[k][i] = GLOBAL ? __ldcg(q + max_rows) : q[max_rows];
+            v[k][i] = GLOBAL ? __ldcg(reinterpret_cast<const float4*>(s + row * D + f)) : *reinterpret_cast<const float4*>(s + row * D + f);
+          }
         }
       }
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
-        const float top = fmaxf(m[k], fmaxf(fmaxf(ms[k][0], ms[k][1]), fmaxf(ms[k][2], ms[k][3]))), base = top == -INFINITY ? 0.0f : top;
+        float top = m[k];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, ms[k][i]);
+        const float base = top == -INFINITY ? 0.0f : top;
         const float c = ex2_approx(m[k] - base);
         m[k] = top;
         l[k] *= c;
         x[k].x *= c; x[k].y *= c; x[k].z *= c; x[k].w *= c;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i0 + i >= members) continue;
-          const float w = ex2_approx(ms[k][i] - base);
+        for (int i = 0; i < AHEAD; ++i) {
+          const float w = ex2_approx(ms[k][i] - base);       // (absent: 0, of zeros)
           l[k] += w * ls[k][i];
           x[k].x += w * v[k][i].x; x[k].y += w * v[k][i].y; x[k].z += w * v[k][i].z; x[k].w += w * v[k][i].w;
         }

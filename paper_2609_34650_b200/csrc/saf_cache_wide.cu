@@ -558,7 +558,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     const Part unit = open_unit[k];
     if (unit.start < 0 || !arrived_s[k]) continue;
     const int first = cut_s.run_of(unit.start), last = cut_s.run_of(unit.last);
-    join<D, ROWS, true, 4>(p, unit, p.max_rows, last - first + 1, [&](int i) { return slot_of(first + i, unit.start); }, nullptr, tid, NT);
+    join<D, ROWS, true, 8, 1>(p, unit, p.max_rows, last - first + 1, [&](int i) { return slot_of(first + i, unit.start); }, nullptr, tid, NT);
   }
 }
 
