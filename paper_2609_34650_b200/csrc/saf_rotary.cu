@@ -14,6 +14,8 @@ namespace saf {
 namespace {
 
 constexpr int ROT_THREADS = 256;
+constexpr int ROT_BLOCKS = 4;       // blocks an SM
+constexpr int ROT_TOKENS = 16;      // tokens of a tile at most
 
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
   const uint4 u = *reinterpret_cast<const uint4*>(p);
@@ -46,30 +48,57 @@ __device__ __forceinline__ void from_f32(__nv_bfloat16* p, float x) { *p = __flo
 __device__ __forceinline__ void from_f32(float* p, float x) { *p = x; }
 
 // A chunk is two vectors of VEC features of one head: VEC pairs below rot_dim, copied features behind it.  VEC = 8 where the
-// halves are whole 8-vectors, else 1.  A thread keeps its chunk (and so its place in the table) and walks rows = (token, head).
+// halves are whole 8-vectors, else 1.  A thread keeps its chunk (and so its place in the table) and walks rows = (token, head).  Four
+// blocks an SM with a row in flight for each thread (forward and backward of 8 x 12 x 4096 x 64: 94 us = 5.3 TB/s; 32768 x 40 heads x 128, 124 us =
+// 5.4; prompts of 31000 tokens into a cache 104 us = 5.4) are as fast as three with two or four rows, and faster than blocks that come and go (98, 129, 127).
 template <typename TI, typename TO, int VEC>
-__global__ void __launch_bounds__(ROT_THREADS) saf_rotary_kernel(RotaryParams p) {
-  extern __shared__ float2 table[];                       // [tokens of the block][rot_dim / 2]: (m cos, m sin)
+__global__ void __launch_bounds__(ROT_THREADS, ROT_BLOCKS) saf_rotary_kernel(const __grid_constant__ RotaryParams p) {
+  extern __shared__ float2 tables[];                      // [2][tokens of a tile][rot_dim / 2]: (m cos, m sin)
+  // element offsets of a token in the five tensors: q, k, v, outputs of q and k (cached step: k's place in its pool), v's place
+  __shared__ long long off_s[2][ROT_TOKENS][6];
+  __shared__ int skip_s[2][ROT_TOKENS];
   pdl_wait();
   pdl_launch_dependents();
-  const int half = p.rot_dim >> 1;
-  const int tok0 = blockIdx.x * p.block_tokens;
-  const int ntok = min(p.block_tokens, p.tokens - tok0);
-  for (int e = threadIdx.x; e < ntok * half; e += ROT_THREADS) {
-    const int tk = e / half, i = e - tk * half;
-    const int n = tok0 + tk;
-    const int pos = p.positions ? p.positions[n] : n % p.T;
-    double turns = static_cast<double>(pos) * (p.freqs[i] * 0.15915494309189535);
-    turns -= rint(turns);
-    float s, c;
-    sincospif(2.0f * static_cast<float>(turns), &s, &c);
-    table[e] = make_float2(c * p.mscale, (p.backward ? -s : s) * p.mscale);
-  }
-  __syncthreads();
+  const int half = p.rot_dim >> 1, TT = p.block_tokens, tiles = (p.tokens - 1) / TT + 1;
+  // what a tile of tokens needs, in one of two places: the next tile's is made while others stream this one
+  auto prepare = [&](int tile, int buf) {
+    const int tok0 = tile * TT, ntok = min(TT, p.tokens - tok0);
+    if (static_cast<int>(threadIdx.x) < ntok) {
+      const int n = tok0 + threadIdx.x;
+      const long long b = n / p.T, t = n - static_cast<int>(b) * p.T;
+      long long* o = off_s[buf][threadIdx.x];
+      o[0] = b * p.q_strides[0] + t * p.q_strides[2];
+      o[1] = b * p.k_strides[0] + t * p.k_strides[2];
+      o[2] = t * p.vn_strides[0];
+      o[3] = b * p.qo_strides[0] + t * p.qo_strides[2];
+      bool skip = false;
+      if (p.slots) {
+        const int slot = p.slots[n];
+        skip = static_cast<unsigned>(slot) >= static_cast<unsigned>(p.n_slots);
+        const long long page = skip ? 0 : slot / p.page_size, place = skip ? 0 : slot - page * p.page_size;
+        o[4] = page * p.ko_strides[0] + place * p.ko_strides[2];
+        o[5] = page * p.vo_strides[0] + place * p.vo_strides[2];
+      } else {
+        o[4] = b * p.ko_strides[0] + t * p.ko_strides[2];
+        o[5] = 0;
+      }
+      skip_s[buf][threadIdx.x] = skip;
+    }
+    float2* table = tables + buf * TT * half;
+    for (int e = threadIdx.x; e < ntok * half; e += ROT_THREADS) {
+      const int tk = e / half, i = e - tk * half;
+      const int n = tok0 + tk;
+      const int pos = p.positions ? p.positions[n] : n % p.T;
+      double turns = static_cast<double>(pos) * (p.freqs[i] * 0.15915494309189535);
+      turns -= rint(turns);
+      float s, c;
+      sincospif(2.0f * static_cast<float>(turns), &s, &c);
+      table[e] = make_float2(c * p.mscale, (p.backward ? -s : s) * p.mscale);
+    }
+  };
   const int chunks = p.D / (2 * VEC), rot_chunks = half / VEC;
   const int subs = ROT_THREADS / chunks;                   // rows that the block handles side by side
   const int chunk = threadIdx.x % chunks, sub = threadIdx.x / chunks;
-  if (sub >= subs) return;
   const bool turning = chunk < rot_chunks;
   int o0, o1;                                              // features of the chunk's two vectors
   if (!turning) {
@@ -83,88 +112,87 @@ __global__ void __launch_bounds__(ROT_THREADS) saf_rotary_kernel(RotaryParams p)
     o1 = half + o0;
   }
   const int heads = p.Hq + p.Hk + p.Hv;
-  int tk = sub / heads, head = sub - tk * heads;
   const int step_t = subs / heads, step_h = subs - step_t * heads;
-  while (tk < ntok) {
-    const int n = tok0 + tk;
-    const long long b = n / p.T, t = n - static_cast<int>(b) * p.T;
-    const TI* src;
-    TO* dst;
-    bool turn = turning;
-    bool skip = false;
-    long long page = 0, place = 0;
-    if (p.slots) {
-      const int slot = p.slots[n];
-      skip = static_cast<unsigned>(slot) >= static_cast<unsigned>(p.n_slots);
-      page = skip ? 0 : slot / p.page_size;
-      place = skip ? 0 : slot - page * p.page_size;
-    }
+  // a row's source and destination
+  auto find = [&](const long long* o, int head, const TI*& src, TO*& dst) {
     if (head < p.Hq) {
-      src = static_cast<const TI*>(p.q) + b * p.q_strides[0] + head * p.q_strides[1] + t * p.q_strides[2];
-      dst = static_cast<TO*>(p.q_out) + b * p.qo_strides[0] + head * p.qo_strides[1] + t * p.qo_strides[2];
+      src = static_cast<const TI*>(p.q) + o[0] + head * p.q_strides[1];
+      dst = static_cast<TO*>(p.q_out) + o[3] + head * p.qo_strides[1];
     } else if (head < p.Hq + p.Hk) {
       const int hk = head - p.Hq;
-      src = static_cast<const TI*>(p.k) + b * p.k_strides[0] + hk * p.k_strides[1] + t * p.k_strides[2];
-      dst = p.slots ? static_cast<TO*>(p.k_out) + page * p.ko_strides[0] + hk * p.ko_strides[1] + place * p.ko_strides[2]
-                    : static_cast<TO*>(p.k_out) + b * p.ko_strides[0] + hk * p.ko_strides[1] + t * p.ko_strides[2];
+      src = static_cast<const TI*>(p.k) + o[1] + hk * p.k_strides[1];
+      dst = static_cast<TO*>(p.k_out) + o[4] + hk * p.ko_strides[1];
     } else {                                               // (new values of a cached step: copied)
       const int hv = head - p.Hq - p.Hk;
-      src = static_cast<const TI*>(p.v) + hv * p.vn_strides[1] + t * p.vn_strides[0];
-      dst = static_cast<TO*>(p.v_out) + page * p.vo_strides[0] + hv * p.vo_strides[1] + place * p.vo_strides[2];
-      turn = false;
+      src = static_cast<const TI*>(p.v) + o[2] + hv * p.vn_strides[1];
+      dst = static_cast<TO*>(p.v_out) + o[5] + hv * p.vo_strides[1];
     }
-    if (!skip) {
-      const float2* row = table + tk * half;
-      if constexpr (VEC == 8) {
-        float a[8], c[8];
-        load8(src + o0, a);
-        load8(src + o1, c);
-        if (turn) {
-          const float4* cs = reinterpret_cast<const float4*>(row + chunk * 8);
-          float x[16];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 u = cs[i];
-            x[4 * i] = u.x; x[4 * i + 1] = u.y; x[4 * i + 2] = u.z; x[4 * i + 3] = u.w;
-          }
-          if (p.interleaved) {
+  };
+  const int tk0 = sub / heads, head0 = sub - tk0 * heads;
+  prepare(blockIdx.x, 0);
+  for (int tile = blockIdx.x, buf = 0; tile < tiles; tile += gridDim.x, buf ^= 1) {
+    __syncthreads();
+    const int ntok = min(TT, p.tokens - tile * TT);
+    const float2* table = tables + buf * TT * half;
+    int tk = sub < subs ? tk0 : ntok, head = head0;
+    while (tk < ntok) {
+      if (!skip_s[buf][tk]) {
+        const TI* src;
+        TO* dst;
+        find(off_s[buf][tk], head, src, dst);
+        const bool turn = turning && head < p.Hq + p.Hk;
+        if constexpr (VEC == 8) {
+          float a[8], c[8];
+          load8(src + o0, a);
+          load8(src + o1, c);
+          if (turn) {
+            const float4* cs = reinterpret_cast<const float4*>(table + tk * half + chunk * 8);
+            float x[16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float a0 = a[2 * i], a1 = a[2 * i + 1], c0 = c[2 * i], c1 = c[2 * i + 1];
-              a[2 * i] = a0 * x[2 * i] - a1 * x[2 * i + 1];
-              a[2 * i + 1] = a1 * x[2 * i] + a0 * x[2 * i + 1];
-              c[2 * i] = c0 * x[8 + 2 * i] - c1 * x[8 + 2 * i + 1];
-              c[2 * i + 1] = c1 * x[8 + 2 * i] + c0 * x[8 + 2 * i + 1];
+              const float4 u = cs[i];
+              x[4 * i] = u.x; x[4 * i + 1] = u.y; x[4 * i + 2] = u.z; x[4 * i + 3] = u.w;
             }
-          } else {
+            if (p.interleaved) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float a0 = a[i], c0 = c[i];
-              a[i] = a0 * x[2 * i] - c0 * x[2 * i + 1];
-              c[i] = c0 * x[2 * i] + a0 * x[2 * i + 1];
+              for (int i = 0; i < 4; ++i) {
+                const float a0 = a[2 * i], a1 = a[2 * i + 1], c0 = c[2 * i], c1 = c[2 * i + 1];
+                a[2 * i] = a0 * x[2 * i] - a1 * x[2 * i + 1];
+                a[2 * i + 1] = a1 * x[2 * i] + a0 * x[2 * i + 1];
+                c[2 * i] = c0 * x[8 + 2 * i] - c1 * x[8 + 2 * i + 1];
+                c[2 * i + 1] = c1 * x[8 + 2 * i] + c0 * x[8 + 2 * i + 1];
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float a0 = a[i], c0 = c[i];
+                a[i] = a0 * x[2 * i] - c0 * x[2 * i + 1];
+                c[i] = c0 * x[2 * i] + a0 * x[2 * i + 1];
+              }
             }
           }
+          store8(dst + o0, a);
+          store8(dst + o1, c);
+        } else {
+          float a = to_f32(src[o0]), c = to_f32(src[o1]);
+          if (turn) {
+            const float2 u = table[tk * half + chunk];
+            const float a0 = a;
+            a = a0 * u.x - c * u.y;
+            c = c * u.x + a0 * u.y;
+          }
+          from_f32(dst + o0, a);
+          from_f32(dst + o1, c);
         }
-        store8(dst + o0, a);
-        store8(dst + o1, c);
-      } else {
-        float a = to_f32(src[o0]), c = to_f32(src[o1]);
-        if (turn) {
-          const float2 u = row[chunk];
-          const float a0 = a;
-          a = a0 * u.x - c * u.y;
-          c = c * u.x + a0 * u.y;
-        }
-        from_f32(dst + o0, a);
-        from_f32(dst + o1, c);
+      }
+      tk += step_t;
+      head += step_h;
+      if (head >= heads) {
+        head -= heads;
+        ++tk;
       }
     }
-    tk += step_t;
-    head += step_h;
-    if (head >= heads) {
-      head -= heads;
-      ++tk;
-    }
+    if (tile + gridDim.x < tiles) prepare(tile + gridDim.x, buf ^ 1);
   }
 }
 
@@ -178,10 +206,13 @@ cudaError_t launch(const RotaryParams& p, int grid, size_t smem, cudaStream_t st
 }  // namespace
 
 cudaError_t launch_rotary(RotaryParams& p, bool in_f32, bool out_f32, int num_sms, cudaStream_t st) {
-  // up to 16 tokens a block (the table: up to 32 KB), as few as give every SM eight blocks
-  p.block_tokens = std::min(16, std::max(1, p.tokens / (8 * num_sms)));
-  const int grid = (p.tokens - 1) / p.block_tokens + 1;
-  const size_t smem = static_cast<size_t>(p.block_tokens) * (p.rot_dim / 2) * sizeof(float2);
+  // tiles of tokens whose table takes up to 8 KB (two of them), on as many blocks as run at once, of a size that gives every
+  // block the same number (32768 tokens on 592 blocks in tiles of 16 were 4 rounds for 3.5: 102 us for 93)
+  const int most = std::max(1, std::min(ROT_TOKENS, 8192 / std::max(4 * p.rot_dim, 1))), blocks = ROT_BLOCKS * num_sms;
+  const int rounds = (p.tokens - 1) / (blocks * most) + 1;
+  p.block_tokens = (p.tokens - 1) / (blocks * rounds) + 1;
+  const int grid = std::min(blocks, (p.tokens - 1) / p.block_tokens + 1);
+  const size_t smem = static_cast<size_t>(2) * p.block_tokens * (p.rot_dim / 2) * sizeof(float2);
   if (in_f32) return out_f32 ? launch<float, float>(p, grid, smem, st) : launch<float, __nv_bfloat16>(p, grid, smem, st);
   return out_f32 ? launch<__nv_bfloat16, float>(p, grid, smem, st) : launch<__nv_bfloat16, __nv_bfloat16>(p, grid, smem, st);
 }
