@@ -38,7 +38,7 @@ __device__ __forceinline__ void load_request(const CacheAttnParams& p, Unit& u) 
 // tiles, with masks, take two to three times the others' time (24 trees of up to 32 tokens on contexts of up to 8192: the slowest block took
 // 1.8 times the mean without).
 template <int ROWS>
-constexpr int EXTRA = ROWS > 16 ? 3 : 0;
+constexpr int EXTRA = ROWS > 16 ? 6 : 0;
 // The next unit that has rows; u.r = p.R behind the last.
 template <int KT, int ROWS>
 __device__ __forceinline__ void next_unit(const CacheAttnParams& p, Unit& u) {

@@ -1,23 +1,25 @@
 // Attention of a step's new tokens over a paged cache where many rows share a key: drafted trees and chains on grouped heads.
 //
 // The mathematics is saf_cache_attn.cu's.  A unit here is one request, one cached head and up to 128 rows (whole new tokens with all
-// query heads of the group, head by head), its tiles 128 keys, and a block takes one run of the line of all tiles.  With 16 rows
+// query heads of the group, head by head), its tiles 64 keys, and a block takes one run of the line of all tiles.  With 16 rows
 // a unit, 128 rows would read the cache eight times out of L2 and issue the 16-row instructions as often; on tcgen05 a tile takes
-// the tensor core about 1000 clk, whatever the rows, of the 2800 that DRAM needs for its 64 KB (head dimension 128).  Two blocks an SM, so that one's
-// chain of scores, softmax and second product runs while the other's waits.
+// the tensor core about 500 clk, whatever the rows, of the 1400 that DRAM needs for its 32 KB (head dimension 128).  The scores of a tile are
+// formed while the one before is in its softmax (two places in TMEM; tiles of 128 keys, for which there is only one, took 7500 clk
+// each in a chain of scores, softmax and second product), and two blocks an SM fill each other's waits.
 //
-// Per block (192 threads): warps 0-3 compute, a thread a row (= TMEM lane) with its 128 scores in registers (two threads a row spilled
-// 700 bytes at the 96 registers that twice the threads leave, and took 10000 clk a tile), warp 4 fetches pages by TMA, warp 5 issues the
-// MMAs and owns TMEM.  TMEM columns [0,128) S (fp32), then weights (bf16 pairs) in [0,64), [128,256) O.  Frozen rows replace their
-// scores by alpha + rho out of a band that is copied in one tile ahead: 128 preferences of keys and 256 of distances for each of
-// up to FZ frozen heads; with more of them, or positions far apart, they take them from global memory.
+// Per block (224 threads): warps 0-3 compute, a thread a row (= TMEM lane; two threads a row spilled 700 bytes at the registers that
+// leaves), warps 4 and 5 fetch pages of keys and of values by TMA (a thread issues a copy in about 300 clk, and pages of 16 tokens
+// take 12 a tile), warp 6 issues the MMAs and owns TMEM.  TMEM columns [0,64) and [64,128) S (fp32) of even and odd tiles, then their
+// weights (bf16 pairs) in the first half of each, [128,256) O.  Frozen rows replace their scores by alpha + rho out of a band that is
+// copied in one tile ahead: 64 preferences of keys and 192 of distances for each of up to FZ frozen heads (up to twice as many:
+// not ahead); with more of them, or positions far apart, they take them from global memory.
 #include "saf_cache_attn.cuh"
 
 namespace saf {
 namespace {
 
-constexpr int ROWS = 128, KT = 128, W = 6, NT = 32 * W, FZ = 4;
-constexpr int SINGLE_TILES = 8;     // tiles up to which a block takes a whole unit where there are no more units than blocks
+constexpr int ROWS = 128, KT = 64, W = 7, NT = 32 * W, FZ = 6, BAND = 256;
+constexpr int SINGLE_TILES = 16;    // tiles up to which a block takes a whole unit where there are no more units than blocks
 constexpr int BLOCKS = 2;           // blocks an SM
 
 template <int D>
@@ -25,10 +27,10 @@ struct Cfg {
   static constexpr int PANELS = D == 64 ? 1 : 2;             // 64 features: 128-byte rows, one swizzle atom
   static constexpr int PANEL = KT * 128;
   static constexpr int TILE = PANELS * PANEL;
-  static constexpr int ST = D == 64 ? 2 : 1;                 // tiles of keys, and of values, in shared memory
-  static constexpr int OFF_Q = 0, OFF_K = TILE, OFF_V = OFF_K + ST * TILE, OFF_TAB = OFF_V + ST * TILE;
-  // words: bands [2][FZ][384], keys' places in a band [2][128], positions of new tokens [64], frozen heads [FZ]
-  static constexpr int TAB = 2 * FZ * 384 + 256 + 64 + FZ;
+  static constexpr int ST = D == 64 ? 4 : 2;                 // tiles of keys, and of values, in shared memory
+  static constexpr int OFF_Q = 0, OFF_K = PANELS * 128 * 128, OFF_V = OFF_K + ST * TILE, OFF_TAB = OFF_V + ST * TILE;
+  // words: bands [2][FZ][BAND], keys' places in a band [2][64], positions of new tokens [64], frozen heads [2 FZ]
+  static constexpr int TAB = 2 * FZ * BAND + 128 + 64 + 2 * FZ;
   static constexpr int SMEM = OFF_TAB + TAB * 4 + 1024;
 };
 
@@ -49,7 +51,7 @@ __device__ __forceinline__ bool wild16(uint32_t w) { return (w & 0x7f80u) == 0x7
 __device__ __noinline__ void slow_scores(const CacheAttnParams& p, const Unit& w, int ctx, int t, int h, int pos, bool keys, bool frozen, uint32_t t_s,
                                          const int* newpos) {
   const int64_t head = static_cast<int64_t>(h) * p.Tp;
-  for (int cc = 0; cc < 8; ++cc) {
+  for (int cc = 0; cc < KT / 16; ++cc) {
     uint32_t r[16];
     if (keys) {
       tmem_ld16(t_s + 16 * cc, r);
@@ -97,35 +99,48 @@ __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint
   return wild;
 }
 
+// The block's part of a unit that lies in several blocks is complete (a barrier lies between its writes and this call, by one thread):
+// whether it is the last.
+__device__ __forceinline__ int arrive(const CacheAttnParams& p, const Cut& cut, const Part& unit) {
+  const int first = cut.run_of(unit.start), last = cut.run_of(unit.last);
+  __threadfence();
+  const bool end = atomicAdd(p.counters + first, 1) == last - first;
+  if (end) p.counters[first] = 0;
+  __threadfence();
+  return end;
+}
+
 template <int D>
 __global__ void __launch_bounds__(NT, BLOCKS)
 saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ CacheAttnParams p) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full, p_full, pv_done, o_free;
+  __shared__ uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2], p_full, pv_done, o_free;
   __shared__ Part open_unit[2];                              // units that go on in other blocks: the run's first, its last
   __shared__ Unit work[2];                                   // what the compute warps are at, in turn
   __shared__ Cut cut_s;
   __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s, frozen_s;
   __shared__ uint32_t tmem_slot;
   float* bands = reinterpret_cast<float*>(smem + C::OFF_TAB);
-  int* places = reinterpret_cast<int*>(bands + 2 * FZ * 384);
-  int* newpos = places + 256;
+  int* places = reinterpret_cast<int*>(bands + 2 * FZ * BAND);
+  int* newpos = places + 128;
   int* fheads = newpos + 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const WaitCtx wc{&abort_s, p.status, p.wait_limit_ns};
   if (tid == 0) {
     abort_s = 0;
     open_unit[0].start = open_unit[1].start = -1;
-    for (int s = 0; s < 2; ++s) {
+    arrived_s[0] = arrived_s[1] = -1;
+    mbar_init(&s_full[0], 1);
+    mbar_init(&s_full[1], 1);
+    for (int s = 0; s < C::ST; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], 1);
       mbar_init(&v_full[s], 1);
       mbar_init(&v_empty[s], 1);
     }
     mbar_init(&q_full, 4);                                   // (one arrival per compute warp)
-    mbar_init(&s_full, 1);
     mbar_init(&p_full, 4);
     mbar_init(&pv_done, 1);
     mbar_init(&o_free, 4);
@@ -161,91 +176,95 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   const int g = p.kv_group;
 
   if (x0 >= x1) {
-  } else if (warp == W - 2) {
-    // ---------------------------------------------------------------- pages
-    uint32_t nk = 0, nv = 0;
-    bool ok = true;
+  } else if (warp == 4 || warp == 5) {
+    // ---------------------------------------------------------------- pages of keys (warp 4) and of values
+    const bool values = warp == 5;
+    uint64_t* full = values ? v_full : k_full;
+    uint64_t* empty = values ? v_empty : k_empty;
+    const CUtensorMap* map = values ? &mv : &mk;
+    uint8_t* ring = smem + (values ? C::OFF_V : C::OFF_K);
     const int br = p.box_rows;
-    constexpr int VB = D == 128 ? 1 : C::PANELS;             // copies of a box of values (128: both halves at once)
+    const int split = values && D == 128 ? 1 : C::PANELS;    // copies of a box (values at 128: both halves at once)
+    uint32_t count = 0;
+    bool ok = true;
     for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
       const int tb = tile_at(u, x0), te = tile_at(u, x1);
-      const bool keys = has_keys(p, u.hk);
-      int ids = 0, ids_at = tb - 4;
-      for (int t = tb; t < te && ok; ++t) {
-        if (t - ids_at >= 4) {                               // lane l: page of the 16 keys number 8 t + l
+      if (!values && !has_keys(p, u.hk)) continue;
+      constexpr int CH = KT / 16;
+      int ids = 0, ids_at = tb - 32 / CH;
+      for (int t = tb; t < te; ++t, ++count) {
+        if (t - ids_at >= 32 / CH) {                         // lane l: page of the 16 keys number CH t + l
           ids_at = t;
-          const int c = t * 8 + lane;
+          const int c = t * CH + lane;
           int id = 0;
           if (c * 16 < max(u.len, 1)) id = p.block_table[static_cast<int64_t>(u.r) * p.max_pages + (p.page_shift >= 0 ? c >> p.page_shift : c / (p.page_size >> 4))];
           ids = min(max(id, 0), p.n_pages - 1);
         }
         const int boxes = min(KT / br, (max(u.len, 1) - t * KT + br - 1) / br);   // (those with keys in them)
-        for (int half = keys ? 0 : 1; half < 2 && ok; ++half) {
-          uint32_t& n = half ? nv : nk;
-          const int s = n % C::ST;
-          uint64_t* full = half ? &v_full[s] : &k_full[s];
-          ok = mbar_wait_warp_compact(half ? &v_empty[s] : &k_empty[s], ((n / C::ST) & 1) ^ 1, wc, half ? SITE_V_EMPTY : SITE_K_EMPTY);
-          if (!ok) break;
-          ++n;
-          const int split = half ? VB : C::PANELS;
-          if (lane == 0) mbar_expect_tx(full, boxes * br * 128 * C::PANELS);
-          uint8_t* dst = smem + (half ? C::OFF_V : C::OFF_K) + s * C::TILE;
-          for (int x = 0; x < boxes * split; ++x) {
-            const int c = split == 2 ? x >> 1 : x, pn = split == 2 ? x & 1 : 0;
-            const int page = __shfl_sync(0xffffffffu, ids, (t - ids_at) * 8 + c * (br >> 4)), at = t * KT + c * br;
-            const int slot = p.page_shift >= 0 ? at & (p.page_size - 1) : at % p.page_size;
-            // keys: panels of 128 rows; values: box after box, its panels one after the other
-            if (lane == 0) tma_load_5d(dst + (half ? (c * C::PANELS + pn) * br * 128 : pn * C::PANEL + c * br * 128), half ? &mv : &mk, full, 64 * pn, slot, 0, u.hk, page);
-          }
-          __syncwarp();
+        const int s = count % C::ST;
+        ok = mbar_wait_warp_compact(&empty[s], ((count / C::ST) & 1) ^ 1, wc, values ? SITE_V_EMPTY : SITE_K_EMPTY);
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(&full[s], boxes * br * 128 * C::PANELS);
+        uint8_t* dst = ring + s * C::TILE;
+        for (int x = 0; x < boxes * split; ++x) {
+          const int c = split == 2 ? x >> 1 : x, pn = split == 2 ? x & 1 : 0;
+          const int page = __shfl_sync(0xffffffffu, ids, (t - ids_at) * CH + c * (br >> 4)), at = t * KT + c * br;
+          const int slot = p.page_shift >= 0 ? at & (p.page_size - 1) : at % p.page_size;
+          // keys: panels of KT rows; values: box after box, its panels one after the other
+          if (lane == 0) tma_load_5d(dst + (values ? (c * C::PANELS + pn) * br * 128 : pn * C::PANEL + c * br * 128), map, &full[s], 64 * pn, slot, 0, u.hk, page);
         }
+        __syncwarp();
       }
     }
   } else if (warp == W - 1) {
     // ---------------------------------------------------------------- MMAs: the whole warp walks, an elected lane issues
     const bool leader = elect_one() != 0;
     const uint32_t sb = smem_u32(smem);
-    constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128, 0, 0), idesc_o = umma_idesc_bf16(128, D, 0, 1);
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, KT, 0, 0), idesc_o = umma_idesc_bf16(128, D, 0, 1);
     const uint64_t d_kmaj = umma_smem_desc(sb, 16, 1024, UMMA_LAYOUT_SW128), d_mn = umma_smem_desc(sb, p.box_rows * 128, 1024, UMMA_LAYOUT_SW128);
     const uint32_t lo_k = desc_lo(d_kmaj), hi_k = desc_hi(d_kmaj), lo_m = desc_lo(d_mn), hi_m = desc_hi(d_mn);
-    uint32_t nq = 0, nk = 0, nv = 0, np = 0, nitem = 0;
+    uint32_t nq = 0, nk = 0, count = 0, nitem = 0;           // count: tiles whose second product has been issued
     bool ok = true;
     const int br = p.box_rows;
     for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
       const int tb = tile_at(u, x0), te = tile_at(u, x1);
       if (tb >= te) continue;
       const bool keys = has_keys(p, u.hk);
+      // scores of the `ahead`-th tile from the one whose second product comes next, into the place of its parity: the weights that were
+      // there have been read by a product issued before
+      auto scores = [&](uint32_t tile) {
+        if (keys) {
+          const int s = nk % C::ST;
+          ok = mbar_wait_warp_compact(&k_full[s], (nk / C::ST) & 1, wc, SITE_K_FULL);
+          if (!ok) return;
+          ++nk;
+          tc_fence_after();
+          if (leader) {
+#pragma unroll
+            for (int kc = 0; kc < D / 16; ++kc)
+              umma_ss2(tmem + KT * (tile & 1), lo_k + ((C::OFF_Q + (kc >> 2) * 128 * 128 + (kc & 3) * 32) >> 4), hi_k,
+                       lo_k + ((C::OFF_K + s * C::TILE + (kc >> 2) * C::PANEL + (kc & 3) * 32) >> 4), hi_k, idesc_s, kc > 0);
+            umma_commit(&k_empty[s]);
+          }
+          __syncwarp();
+        }
+        if (leader) umma_commit(&s_full[tile & 1]);          // (without keys too: one phase a tile)
+        __syncwarp();
+      };
       if (keys) {
         ok = mbar_wait_warp_compact(&q_full, nq & 1, wc, SITE_Q_FULL);
         if (!ok) break;
         ++nq;
       }
+      scores(count);
       for (int t = tb; t < te && ok; ++t) {
-        if (keys) {
-          const int s = nk % C::ST;
-          ok = mbar_wait_warp_compact(&k_full[s], (nk / C::ST) & 1, wc, SITE_K_FULL);
-          if (!ok) break;
-          ++nk;
-          tc_fence_after();
-          if (leader) {
-#pragma unroll
-            for (int kc = 0; kc < D / 16; ++kc) {
-              const uint32_t off = ((kc >> 2) * C::PANEL + (kc & 3) * 32) >> 4;
-              umma_ss2(tmem, lo_k + (C::OFF_Q >> 4) + off, hi_k, lo_k + ((C::OFF_K + s * C::TILE) >> 4) + off, hi_k, idesc_s, kc > 0);
-            }
-            umma_commit(&k_empty[s]);
-          }
-          __syncwarp();
-        }
-        if (leader) umma_commit(&s_full);                    // (without keys too: one phase a tile)
-        __syncwarp();
-        ok = mbar_wait_warp_compact(&p_full, np & 1, wc, SITE_P_FULL);
+        if (t + 1 < te) scores(count + 1);
         if (!ok) break;
-        ++np;
-        const int s = nv % C::ST;
-        ok = mbar_wait_warp_compact(&v_full[s], (nv / C::ST) & 1, wc, SITE_V_FULL);
+        ok = mbar_wait_warp_compact(&p_full, count & 1, wc, SITE_P_FULL);
         if (!ok) break;
-        ++nv;
+        const int s = count % C::ST;
+        ok = mbar_wait_warp_compact(&v_full[s], (count / C::ST) & 1, wc, SITE_V_FULL);
+        if (!ok) break;
         if (t == tb) {
           ok = mbar_wait_warp_compact(&o_free, (nitem & 1) ^ 1, wc, SITE_O_FREE);
           if (!ok) break;
@@ -253,13 +272,14 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         tc_fence_after();
         if (leader) {
 #pragma unroll
-          for (int kc = 0; kc < 8; ++kc)
-            umma_ts2(tmem + 128, tmem + 8 * kc,
+          for (int kc = 0; kc < KT / 16; ++kc)
+            umma_ts2(tmem + 128, tmem + KT * (count & 1) + 8 * kc,
                      lo_m + ((C::OFF_V + s * C::TILE + ((kc * 16 / br) * C::PANELS * br + kc * 16 % br) * 128) >> 4), hi_m, idesc_o, kc > 0 || t > tb ? 1u : 0u);
           umma_commit(&v_empty[s]);
           umma_commit(&pv_done);
         }
         __syncwarp();
+        ++count;
       }
       ++nitem;
     }
@@ -280,6 +300,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         range_s[k & 1][1] = more ? tile_at(v, x1) : -1;
       }
       if (named_bar_or(5, 128, !ok)) break;
+      if (tid == 0 && k == 1 && open_unit[0].start >= 0) arrived_s[0] = arrive(p, cut_s, open_unit[0]);   // (the first unit's part is complete)
       const int tb = range_s[k & 1][0], te = range_s[k & 1][1];
       if (te < 0) break;
       const Unit& w = work[k & 1];
@@ -294,12 +315,12 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       if (keys) {
         // queries of ordinary rows, zeros elsewhere, as the swizzled tile that TMA would leave
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(n) * p.q_strides[0] + h * p.q_strides[1];
-        const uint32_t base = smem_u32(smem) + C::OFF_Q + tid * 128;
+        const uint32_t base = smem_u32(smem) + C::OFF_Q + tid * 128;   // (panels of 128 rows)
         uint4 x[D / 8];
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) x[c] = there && !frozen ? *reinterpret_cast<const uint4*>(q + c * 8) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) st_shared_v4w(base + (c >> 3) * C::PANEL + (((c & 7) ^ (tid & 7)) << 4), x[c].x, x[c].y, x[c].z, x[c].w);
+        for (int c = 0; c < D / 8; ++c) st_shared_v4w(base + (c >> 3) * 128 * 128 + (((c & 7) ^ (tid & 7)) << 4), x[c].x, x[c].y, x[c].z, x[c].w);
         fence_proxy_async_smem();
         warp_arrive(&q_full);
       }
@@ -309,7 +330,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         for (int c = 0; c < g; ++c) {
           const int hk = w.hk * g + c;
           if ((p.frozen[hk >> 5] >> (hk & 31)) & 1) {
-            if (found < FZ) fheads[found] = hk;
+            if (found < 2 * FZ) fheads[found] = hk;
             ++found;
           }
         }
@@ -319,7 +340,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       if (tid < w.many) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
       named_bar_sync(6, 128);
       const int n_frozen = frozen_s;
-      bool any_frozen = false, fast = false;
+      bool any_frozen = false, fast = false, ahead = false;
       uint32_t band_at = 0;                                  // this row's band: alpha of key 0
       int rho_at = 0;                                        // from there to rho of that key
       int pos = 0, pmin = 0;
@@ -333,61 +354,69 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         }
         pmin = __reduce_min_sync(0xffffffffu, lo);
         const int span = __reduce_max_sync(0xffffffffu, hi) - pmin;
-        fast = n_frozen <= FZ && pmin >= ctx && span < 64 && ctx >= 0;
+        fast = n_frozen <= 2 * FZ && pmin >= ctx && span < 64 && ctx >= 0;
+        ahead = fast && n_frozen <= FZ;
         if (frozen && p.positions) {                         // (new tokens behind the row's position are not seen)
           for (int c = 0; c < w.many; ++c)
             if (newpos[c] > pos) mask &= ~(1ull << c);
         }
         int slot = 0;
-        for (int c = 0; c < min(n_frozen, FZ); ++c)
+        for (int c = 0; c < min(n_frozen, 2 * FZ); ++c)
           if (fheads[c] == h) slot = c;
-        band_at = smem_u32(bands + slot * 384);
-        rho_at = (128 + min(max(pos - pmin, 0), 63) + 127) * 4;
+        band_at = smem_u32(bands + slot * BAND);
+        rho_at = (KT + min(max(pos - pmin, 0), 63) + KT - 1) * 4;
         any_frozen = __any_sync(0xffffffffu, frozen && there);
       }
-      // A tile's band: alpha of its keys' positions, then rho of distances pmin - (j0 + 127) and up (what lies outside the vectors
+      // A tile's band: alpha of its keys' positions, then rho of distances pmin - (j0 + KT - 1) and up (what lies outside the vectors
       // belongs to keys that are not seen).
       auto fetch_band = [&](int t) {
-        const int j = t * KT + tid, at = j < ctx ? j : j < w.len ? newpos[j - ctx] : -1, d = pmin - t * KT - 127 + tid;
-        if (j - tid + KT > ctx) places[(t & 1) * 128 + tid] = 4 * min(max(at < 0 ? tid : at - t * KT, -63), 127);   // (new tokens lie at their positions)
-        uint32_t dst = smem_u32(bands + (t & 1) * FZ * 384 + tid);
-        for (int c = 0; c < n_frozen; ++c, dst += 384 * 4) {
+        const int buf = ahead ? t & 1 : 0, j0 = t * KT;
+        uint32_t dst = smem_u32(bands + buf * FZ * BAND + tid);
+        const bool key = tid < KT;
+        const int j = j0 + tid, at = !key ? pmin - j0 - (KT - 1) + tid - KT : j < ctx ? j : j < w.len ? newpos[j - ctx] : -1, d1 = pmin - j0 + 1 + tid;
+        if (key && j0 + KT > ctx) places[buf * KT + tid] = 4 * min(max(at < 0 ? tid : at - j0, -63), KT - 1);   // (new tokens lie at their positions)
+        const bool in0 = at >= 0 && at < p.Tp, in1 = d1 >= 0 && d1 < p.Tp;
+        const float* src = key ? p.alpha : p.rho;
+        for (int c = 0; c < n_frozen; ++c, dst += BAND * 4) {
           const int64_t head = static_cast<int64_t>(fheads[c]) * p.Tp;
-          copy4(dst, p.alpha + head + max(at, 0), at >= 0);
-          const bool in0 = d >= 0 && d < p.Tp, in1 = d + 128 >= 0 && d + 128 < p.Tp;
-          copy4(dst + 128 * 4, p.rho + head + (in0 ? d : 0), in0);
-          copy4(dst + 256 * 4, p.rho + head + (in1 ? d + 128 : 0), in1);
+          copy4(dst, src + head + (in0 ? at : 0), in0);
+          copy4(dst + 128 * 4, p.rho + head + (in1 ? d1 : 0), in1);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      if (fast) fetch_band(tb);
+      if (ahead) fetch_band(tb);
       const float cf = frozen ? LOG2E : p.scale_log2;         // from scores to powers of two
       float m_ref = -INFINITY, l = 0.0f;
       for (int t = tb; t < te; ++t, ++count) {
         const bool plain = (t + 1) * KT <= ctx;               // all of its keys were cached before the step
         if (fast) {
+          if (!ahead) {
+            named_bar_sync(6, 128);                           // (the band of the tile before has been read)
+            fetch_band(t);
+          }
           asm volatile("cp.async.wait_all;" ::: "memory");
           named_bar_sync(6, 128);                             // (the band of this tile is there, that of the one before has been read)
-          if (t + 1 < te) fetch_band(t + 1);
+          if (ahead && t + 1 < te) fetch_band(t + 1);
         }
-        if (!mbar_wait_warp_compact(&s_full, count & 1, wc, SITE_S_FULL)) ok = false;
-        if (t > tb && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
+        const uint32_t t_p = t_s + KT * (count & 1);
+        if (!mbar_wait_warp_compact(&s_full[count & 1], (count >> 1) & 1, wc, SITE_S_FULL)) ok = false;
         tc_fence_after();
+        float m_new = m_ref;
         if (!idle) {
-          if (any_frozen && !fast) slow_scores(p, w, ctx, t, h, pos, keys, frozen, t_s, newpos);
+          if (any_frozen && !fast) slow_scores(p, w, ctx, t, h, pos, keys, frozen, t_p, newpos);
           // 32 scores at a time, so that loads have registers to arrive in: first the maximum (what differs from the MMA's scores is
           // written back), then the weights
           const bool written = (any_frozen && fast) || !plain;
           float top = -INFINITY;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {                       // (not unrolled: the loop over tiles has to stay in the instruction cache)
+          for (int c = 0; c < KT / 32; ++c) {                 // (not unrolled: the loop over tiles has to stay in the instruction cache)
             uint32_t r[32];
             if (keys || !fast) {
-              tmem_ld32(t_s + 32 * c, r);
+              tmem_ld32(t_p + 32 * c, r);
               tmem_wait_ld();
             }
             if (any_frozen && fast) {
-              const uint32_t a = band_at + (t & 1) * (FZ * 384 * 4) + 128 * c;
+              const uint32_t a = band_at + (ahead ? t & 1 : 0) * (FZ * BAND * 4) + 128 * c;
               if (plain) {
                 float x[32], y[32];
 #pragma unroll
@@ -399,7 +428,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
                   if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
               } else {
                 float x[32], y[32];
-                const uint32_t pl = smem_u32(places + (t & 1) * 128 + 32 * c);
+                const uint32_t pl = smem_u32(places + (ahead ? t & 1 : 0) * KT + 32 * c);
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
                   ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -420,7 +449,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               for (int e = 0; e < 32; ++e)
                 if (!((sees >> e) & 1)) r[e] = 0xff800000u;
             }
-            if (written) tmem_st32(t_s + 32 * c, r);
+            if (written) tmem_st32(t_p + 32 * c, r);
             float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
@@ -430,12 +459,16 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             top = max3(top, mx0, mx1);
           }
           if (written) tmem_wait_st();
+          m_new = fmaxf(m_ref, top * cf);
+        }
+        if (t > tb && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
+        if (!idle) {
           // the reference follows the maximum where that has grown by more than 2^8
-          const float m_new = fmaxf(m_ref, top * cf);
           const bool need = m_new - m_ref > 8.0f;             // (from -inf: always; -inf to -inf: NaN, no)
           if (t == tb) {
             m_ref = m_new;
           } else if (__any_sync(0xffffffffu, need)) {
+            tc_fence_after();
             const float f = need ? ex2_approx(m_ref - m_new) : 1.0f;
             l *= f;
             if (need) m_ref = m_new;
@@ -452,9 +485,9 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           const float neg_m = m_ref == -INFINITY ? 0.0f : -m_ref;
           float sum[2] = {0.0f, 0.0f};
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {                       // (the weights of 32 keys take the place of scores that have been read)
+          for (int c = 0; c < KT / 32; ++c) {                 // (the weights of 32 keys take the place of scores that have been read)
             uint32_t r[32], pk[16];
-            tmem_ld32(t_s + 32 * c, r);
+            tmem_ld32(t_p + 32 * c, r);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -463,7 +496,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               sum[1] += a1;
               pk[e] = pack_bf16x2(a0, a1);
             }
-            tmem_st16(t_s + 16 * c, pk);
+            tmem_st16(t_p + 16 * c, pk);
           }
           l += sum[0] + sum[1];
         }
@@ -544,20 +577,14 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   __syncthreads();
   if (warp == W - 1) tmem_dealloc(tmem, 256);
   if (open_unit[0].start < 0 && open_unit[1].start < 0) return;
-  if (tid < 2 && open_unit[tid].start >= 0) {
-    const Part& unit = open_unit[tid];
-    const int first = cut_s.run_of(unit.start), last = cut_s.run_of(unit.last);
-    __threadfence();                                          // (the block's parts, which the barrier put before this)
-    const bool end = atomicAdd(p.counters + first, 1) == last - first;
-    if (end) p.counters[first] = 0;
-    arrived_s[tid] = end;
-    __threadfence();
-  }
+  if (tid < 2 && open_unit[tid].start >= 0 && arrived_s[tid] < 0) arrived_s[tid] = arrive(p, cut_s, open_unit[tid]);
   __syncthreads();
+  // (a run's first unit has mostly been reported long before, so that its other blocks join it and this one its last)
   for (int k = 0; k < 2; ++k) {
     const Part unit = open_unit[k];
-    if (unit.start < 0 || !arrived_s[k]) continue;
+    if (unit.start < 0 || arrived_s[k] != 1) continue;
     const int first = cut_s.run_of(unit.start), last = cut_s.run_of(unit.last);
+    __threadfence();
     join<D, ROWS, true, 8, 1>(p, unit, p.max_rows, last - first + 1, [&](int i) { return slot_of(first + i, unit.start); }, nullptr, tid, NT);
   }
 }
