@@ -7,18 +7,18 @@
 // formed while the one before is in its softmax (two places in TMEM; tiles of 128 keys, for which there is only one, took 7500 clk
 // each in a chain of scores, softmax and second product), and two blocks an SM fill each other's waits.
 //
-// Per block (224 threads): warps 0-3 compute, a thread a row (= TMEM lane; two threads a row spilled 700 bytes at the registers that
+// Per block (256 threads): warps 0-3 compute, a thread a row (= TMEM lane; two threads a row spilled 700 bytes at the registers that
 // leaves), warps 4 and 5 fetch pages of keys and of values by TMA (a thread issues a copy in about 300 clk, and pages of 16 tokens
-// take 12 a tile), warp 6 issues the MMAs and owns TMEM.  TMEM columns [0,64) and [64,128) S (fp32) of even and odd tiles, then their
+// take 12 a tile), warp 6 issues the MMAs and owns TMEM, warp 7 fetches bands.  TMEM columns [0,64) and [64,128) S (fp32) of even and odd tiles, then their
 // weights (bf16 pairs) in the first half of each, [128,256) O.  Frozen rows replace their scores by alpha + rho out of a band that is
-// copied in one tile ahead: 64 preferences of keys and 192 of distances for each of up to FZ frozen heads (up to twice as many:
-// not ahead); with more of them, or positions far apart, they take them from global memory.
+// copied in ahead: 64 preferences of keys and 192 of distances for each of up to FZ frozen heads (up to twice as many
+// in one place instead of two); with more of them, or positions far apart, they take them from global memory.
 #include "saf_cache_attn.cuh"
 
 namespace saf {
 namespace {
 
-constexpr int ROWS = 128, KT = 64, W = 7, NT = 32 * W, FZ = 6, BAND = 256;
+constexpr int ROWS = 128, KT = 64, W = 8, NT = 32 * W, FZ = 6, BAND = 256;
 constexpr int SINGLE_TILES = 16;    // tiles up to which a block takes a whole unit where there are no more units than blocks
 constexpr int BLOCKS = 2;           // blocks an SM
 
@@ -29,12 +29,12 @@ struct Cfg {
   static constexpr int TILE = PANELS * PANEL;
   static constexpr int ST = D == 64 ? 4 : 2;                 // tiles of keys, and of values, in shared memory
   static constexpr int OFF_Q = 0, OFF_K = PANELS * 128 * 128, OFF_V = OFF_K + ST * TILE, OFF_TAB = OFF_V + ST * TILE;
-  // words: bands [2][FZ][BAND], keys' places in a band [2][64], positions of new tokens [64], frozen heads [2 FZ]
-  static constexpr int TAB = 2 * FZ * BAND + 128 + 64 + 2 * FZ;
+  // words: bands [2][FZ][BAND], keys' places in a band [2][64], positions of new tokens [64]
+  static constexpr int TAB = 2 * FZ * BAND + 128 + 64;
   static constexpr int SMEM = OFF_TAB + TAB * 4 + 1024;
 };
 
-enum WideSite { SITE_K_EMPTY = 111, SITE_V_EMPTY, SITE_Q_FULL, SITE_K_FULL, SITE_P_FULL, SITE_V_FULL, SITE_O_FREE, SITE_S_FULL, SITE_PV_DONE };
+enum WideSite { SITE_K_EMPTY = 111, SITE_V_EMPTY, SITE_Q_FULL, SITE_K_FULL, SITE_P_FULL, SITE_V_FULL, SITE_O_FREE, SITE_S_FULL, SITE_PV_DONE, SITE_BAND_EMPTY, SITE_BAND_FULL };
 
 // 4 bytes, or zeros
 __device__ __forceinline__ void copy4(uint32_t dst, const float* src, bool in) {
@@ -99,6 +99,32 @@ __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint
   return wild;
 }
 
+// Whether and how a unit's frozen rows go by bands; by a whole warp, the same for all.
+struct BandPlan {
+  int n_frozen, pmin, span;
+  bool fast, ahead;                 // by bands; in two places in turn
+};
+__device__ __forceinline__ BandPlan plan_band(const CacheAttnParams& p, const Unit& w) {
+  BandPlan b{0, 0, 0, false, false};
+  for (int c = 0; c < p.kv_group; ++c) {
+    const int hk = w.hk * p.kv_group + c;
+    b.n_frozen += (p.frozen[hk >> 5] >> (hk & 31)) & 1;
+  }
+  if (b.n_frozen == 0) return b;
+  const int ctx = w.len - w.many, t0 = w.rt * p.tile_tokens, t1 = min(t0 + p.tile_tokens, w.many);
+  int lo = 0x7fffffff, hi = 0;
+  for (int c = t0 + (threadIdx.x & 31); c < t1; c += 32) {
+    const int x = p.positions ? min(max(p.positions[w.first + c], 0), p.Tp - 1) : max(ctx + c, 0);
+    lo = min(lo, x);
+    hi = max(hi, x);
+  }
+  b.pmin = __reduce_min_sync(0xffffffffu, lo);
+  b.span = __reduce_max_sync(0xffffffffu, hi) - b.pmin;
+  b.fast = b.n_frozen <= 2 * FZ && b.pmin >= ctx && b.span < 64 && ctx >= 0;
+  b.ahead = b.fast && b.n_frozen <= FZ;
+  return b;
+}
+
 // The block's part of a unit that lies in several blocks is complete (a barrier lies between its writes and this call, by one thread):
 // whether it is the last.
 __device__ __forceinline__ int arrive(const CacheAttnParams& p, const Cut& cut, const Part& unit) {
@@ -116,24 +142,26 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2], p_full, pv_done, o_free;
+  __shared__ uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2], p_full, pv_done, o_free, band_full[2], band_empty[2];
   __shared__ Part open_unit[2];                              // units that go on in other blocks: the run's first, its last
   __shared__ Unit work[2];                                   // what the compute warps are at, in turn
   __shared__ Cut cut_s;
-  __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s, frozen_s;
+  __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s;
   __shared__ uint32_t tmem_slot;
   float* bands = reinterpret_cast<float*>(smem + C::OFF_TAB);
   int* places = reinterpret_cast<int*>(bands + 2 * FZ * BAND);
   int* newpos = places + 128;
-  int* fheads = newpos + 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const WaitCtx wc{&abort_s, p.status, p.wait_limit_ns};
   if (tid == 0) {
     abort_s = 0;
     open_unit[0].start = open_unit[1].start = -1;
     arrived_s[0] = arrived_s[1] = -1;
-    mbar_init(&s_full[0], 1);
-    mbar_init(&s_full[1], 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&band_full[s], 64);                          // (each lane's copies, and each lane)
+      mbar_init(&band_empty[s], 4);
+    }
     for (int s = 0; s < C::ST; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], 1);
@@ -148,7 +176,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     tma_prefetch_desc(&mk);
     tma_prefetch_desc(&mv);
   }
-  if (warp == W - 1) {
+  if (warp == 6) {
     tmem_alloc(&tmem_slot, 256);
     tmem_relinquish();
   }
@@ -216,7 +244,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         __syncwarp();
       }
     }
-  } else if (warp == W - 1) {
+  } else if (warp == 6) {
     // ---------------------------------------------------------------- MMAs: the whole warp walks, an elected lane issues
     const bool leader = elect_one() != 0;
     const uint32_t sb = smem_u32(smem);
@@ -283,10 +311,58 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       }
       ++nitem;
     }
+  } else if (warp == 7) {
+    // ---------------------------------------------------------------- bands.  A tile's: alpha of its keys' positions, then rho of distances
+    // pmin - (j0 + KT - 1) and up (what lies outside the vectors belongs to keys that are not seen)
+    uint32_t used[2] = {0, 0};
+    bool ok = true;
+    for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
+      const int tb = tile_at(u, x0), te = tile_at(u, x1);
+      if (tb >= te) continue;
+      const BandPlan b = plan_band(p, u);
+      if (!b.fast) continue;
+      const int ctx = u.len - u.many;
+      for (int s = 0; s < 2 && ok; ++s) ok = mbar_wait_warp_compact(&band_empty[s], (used[s] & 1) ^ 1, wc, SITE_BAND_EMPTY);
+      for (int t = tb; t < te && ok; ++t) {
+        const int buf = b.ahead ? (t - tb) & 1 : 0, j0 = t * KT;
+        ok = mbar_wait_warp_compact(&band_empty[buf], (used[buf] & 1) ^ 1, wc, SITE_BAND_EMPTY);
+        if (!ok) break;
+        ++used[buf];
+        int at[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int y = lane + 32 * i, j = j0 + y;
+          at[i] = j < ctx ? j : j >= u.len ? -1 : p.positions ? min(max(p.positions[u.first + j - ctx], 0), p.Tp - 1) : j;
+          if (j0 + KT > ctx) places[buf * KT + y] = 4 * min(max(at[i] < 0 ? y : at[i] - j0, -63), KT - 1);   // (new tokens lie at their positions)
+        }
+        uint32_t dst = smem_u32(bands + buf * FZ * BAND + lane);
+        const int d0 = b.pmin - j0 - (KT - 1) + lane;
+        int seen = 0;
+        for (int c = 0; c < g; ++c) {
+          const int hk = u.hk * g + c;
+          if (!((p.frozen[hk >> 5] >> (hk & 31)) & 1)) continue;
+          const int64_t head = static_cast<int64_t>(hk) * p.Tp;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) copy4(dst + 128 * i, p.alpha + head + max(at[i], 0), at[i] >= 0);
+#pragma unroll
+          for (int i = 0; i < 6; ++i) {
+            const int d = d0 + 32 * i;
+            const bool in = d >= 0 && d < p.Tp;
+            copy4(dst + 256 + 128 * i, p.rho + head + (in ? d : 0), in);
+          }
+          dst += BAND * 4;
+          if (++seen == b.n_frozen) break;
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&band_full[buf])) : "memory");
+        mbar_arrive(&band_full[buf]);
+      }
+    }
+    // (copies in flight land before the block ends)
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     // ---------------------------------------------------------------- softmax
     const uint32_t t_s = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-    uint32_t count = 0;                                      // tiles so far
+    uint32_t count = 0, band0 = 0, band1 = 0;                // tiles so far; bands, in either place
     bool ok = true;
     // (a warp whose wait was abandoned walks on, without storing, until all four leave together)
     for (uint32_t k = 0;; ++k) {
@@ -324,80 +400,34 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         fence_proxy_async_smem();
         warp_arrive(&q_full);
       }
-      // frozen heads of the group, positions of the new tokens
-      if (tid == 0) {
-        int found = 0;
-        for (int c = 0; c < g; ++c) {
-          const int hk = w.hk * g + c;
-          if ((p.frozen[hk >> 5] >> (hk & 31)) & 1) {
-            if (found < 2 * FZ) fheads[found] = hk;
-            ++found;
-          }
-        }
-        frozen_s = found;
-        wild_s = 0;
-      }
+      if (tid == 0) wild_s = 0;
       if (tid < w.many) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
       named_bar_sync(6, 128);
-      const int n_frozen = frozen_s;
-      bool any_frozen = false, fast = false, ahead = false;
+      const BandPlan plan = plan_band(p, w);
+      const bool fast = plan.fast;
+      bool any_frozen = false;
       uint32_t band_at = 0;                                  // this row's band: alpha of key 0
       int rho_at = 0;                                        // from there to rho of that key
-      int pos = 0, pmin = 0;
-      if (n_frozen > 0) {
+      int pos = 0;
+      if (plan.n_frozen > 0) {
         pos = newpos[i];
-        int lo = 0x7fffffff, hi = 0;
-        for (int c = lane; c < rows / g; c += 32) {
-          const int x = newpos[w.rt * p.tile_tokens + c];
-          lo = min(lo, x);
-          hi = max(hi, x);
-        }
-        pmin = __reduce_min_sync(0xffffffffu, lo);
-        const int span = __reduce_max_sync(0xffffffffu, hi) - pmin;
-        fast = n_frozen <= 2 * FZ && pmin >= ctx && span < 64 && ctx >= 0;
-        ahead = fast && n_frozen <= FZ;
         if (frozen && p.positions) {                         // (new tokens behind the row's position are not seen)
           for (int c = 0; c < w.many; ++c)
             if (newpos[c] > pos) mask &= ~(1ull << c);
         }
-        int slot = 0;
-        for (int c = 0; c < min(n_frozen, 2 * FZ); ++c)
-          if (fheads[c] == h) slot = c;
-        band_at = smem_u32(bands + slot * BAND);
-        rho_at = (KT + min(max(pos - pmin, 0), 63) + KT - 1) * 4;
+        int slot = 0;                                        // frozen heads of the group before this one
+        for (int c = 0; c < hg; ++c) slot += (p.frozen[(w.hk * g + c) >> 5] >> ((w.hk * g + c) & 31)) & 1;
+        if (!frozen) slot = 0;
+        band_at = smem_u32(bands + min(slot, 2 * FZ - 1) * BAND);
+        rho_at = (KT + min(max(pos - plan.pmin, 0), 63) + KT - 1) * 4;
         any_frozen = __any_sync(0xffffffffu, frozen && there);
       }
-      // A tile's band: alpha of its keys' positions, then rho of distances pmin - (j0 + KT - 1) and up (what lies outside the vectors
-      // belongs to keys that are not seen).
-      auto fetch_band = [&](int t) {
-        const int buf = ahead ? t & 1 : 0, j0 = t * KT;
-        uint32_t dst = smem_u32(bands + buf * FZ * BAND + tid);
-        const bool key = tid < KT;
-        const int j = j0 + tid, at = !key ? pmin - j0 - (KT - 1) + tid - KT : j < ctx ? j : j < w.len ? newpos[j - ctx] : -1, d1 = pmin - j0 + 1 + tid;
-        if (key && j0 + KT > ctx) places[buf * KT + tid] = 4 * min(max(at < 0 ? tid : at - j0, -63), KT - 1);   // (new tokens lie at their positions)
-        const bool in0 = at >= 0 && at < p.Tp, in1 = d1 >= 0 && d1 < p.Tp;
-        const float* src = key ? p.alpha : p.rho;
-        for (int c = 0; c < n_frozen; ++c, dst += BAND * 4) {
-          const int64_t head = static_cast<int64_t>(fheads[c]) * p.Tp;
-          copy4(dst, src + head + (in0 ? at : 0), in0);
-          copy4(dst + 128 * 4, p.rho + head + (in1 ? d1 : 0), in1);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      };
-      if (ahead) fetch_band(tb);
       const float cf = frozen ? LOG2E : p.scale_log2;         // from scores to powers of two
       float m_ref = -INFINITY, l = 0.0f;
       for (int t = tb; t < te; ++t, ++count) {
         const bool plain = (t + 1) * KT <= ctx;               // all of its keys were cached before the step
-        if (fast) {
-          if (!ahead) {
-            named_bar_sync(6, 128);                           // (the band of the tile before has been read)
-            fetch_band(t);
-          }
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          named_bar_sync(6, 128);                             // (the band of this tile is there, that of the one before has been read)
-          if (ahead && t + 1 < te) fetch_band(t + 1);
-        }
+        const int buf = plan.ahead ? (t - tb) & 1 : 0;
+        if (fast && !mbar_wait_warp_compact(&band_full[buf], (buf ? band1 : band0) & 1, wc, SITE_BAND_FULL)) ok = false;
         const uint32_t t_p = t_s + KT * (count & 1);
         if (!mbar_wait_warp_compact(&s_full[count & 1], (count >> 1) & 1, wc, SITE_S_FULL)) ok = false;
         tc_fence_after();
@@ -416,7 +446,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               tmem_wait_ld();
             }
             if (any_frozen && fast) {
-              const uint32_t a = band_at + (ahead ? t & 1 : 0) * (FZ * BAND * 4) + 128 * c;
+              const uint32_t a = band_at + buf * (FZ * BAND * 4) + 128 * c;
               if (plain) {
                 float x[32], y[32];
 #pragma unroll
@@ -428,7 +458,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
                   if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
               } else {
                 float x[32], y[32];
-                const uint32_t pl = smem_u32(places + (ahead ? t & 1 : 0) * KT + 32 * c);
+                const uint32_t pl = smem_u32(places + buf * KT + 32 * c);
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
                   ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -460,6 +490,11 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           }
           if (written) tmem_wait_st();
           m_new = fmaxf(m_ref, top * cf);
+        }
+        if (fast) {                                           // (the band has been read)
+          warp_arrive(&band_empty[buf]);
+          if (buf) ++band1;
+          else ++band0;
         }
         if (t > tb && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
         if (!idle) {
@@ -575,7 +610,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == W - 1) tmem_dealloc(tmem, 256);
+  if (warp == 6) tmem_dealloc(tmem, 256);
   if (open_unit[0].start < 0 && open_unit[1].start < 0) return;
   if (tid < 2 && open_unit[tid].start >= 0 && arrived_s[tid] < 0) arrived_s[tid] = arrive(p, cut_s, open_unit[tid]);
   __syncthreads();
