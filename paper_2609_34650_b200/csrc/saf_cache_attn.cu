@@ -589,7 +589,8 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
   p.stages = static_cast<int>(std::min<size_t>(MAX_STAGES, (room - parts) / ring));
   const size_t smem = p.stages * ring + parts + 1024;
   auto kernel = p.o_f32 ? saf_cache_attn_kernel<D, NB, true> : saf_cache_attn_kernel<D, NB, false>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  static SmemLimit limits[2];
+  const cudaError_t e = raise_smem(kernel, static_cast<int>(room) + 1024, limits[p.o_f32 ? 1 : 0]);
   if (e != cudaSuccess) return e;
   return launch_pdl(PDL_REST, kernel, num_sms, 32 * W, smem, st, mk, mv, p);
 }

@@ -626,7 +626,8 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 
 template <int D>
 cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnParams& p, int num_sms, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(saf_cache_wide_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
+  static SmemLimit limit;
+  const cudaError_t e = raise_smem(saf_cache_wide_kernel<D>, Cfg<D>::SMEM, limit);
   if (e != cudaSuccess) return e;
   return launch_pdl(PDL_REST, saf_cache_wide_kernel<D>, BLOCKS * num_sms, NT, Cfg<D>::SMEM, st, mk, mv, p);
 }

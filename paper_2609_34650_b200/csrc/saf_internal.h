@@ -3,6 +3,7 @@
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <atomic>
 #include <cstdlib>
 #include <utility>
 
@@ -34,6 +35,18 @@ inline int pdl_mask() {
   return m;
 }
 enum { PDL_STAGE = 1, PDL_FWD = 2, PDL_PREP = 4, PDL_BWD = 8, PDL_FWD128 = 16, PDL_PREP_SMALL = 32, PDL_REST = 64 };
+// Raises a kernel's limit of dynamic shared memory, once for each device (`limit`: one a kernel, which always asks for the same
+// size, so that threads that meet here do no harm).  Devices beyond the array ask each time.
+struct SmemLimit { std::atomic<int> bytes[16] = {}; };
+template <typename... KArgs>
+cudaError_t raise_smem(void (*kernel)(KArgs...), int bytes, SmemLimit& limit) {
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev >= 0 && dev < 16 && limit.bytes[dev] >= bytes)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 16) limit.bytes[dev] = bytes;
+  return e;
+}
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl(int which, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
