@@ -569,22 +569,36 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               }
             }
           }
-          if (there && ok && whole) {
-            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.O) + static_cast<int64_t>(n) * p.o_strides[0] + h * p.o_strides[1] + f0;
+          // a warp's 32 rows by way of its share of the queries' place, so that a store covers whole lines (row by row they took 20000 clk a
+          // part)
+          const uint32_t stage = smem_u32(smem) + C::OFF_Q + warp * 4096;
+          if (whole) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              st_shared_v4w(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), pack_bf16x2(__uint_as_float(r[8 * c]) * inv, __uint_as_float(r[8 * c + 1]) * inv),
+                            pack_bf16x2(__uint_as_float(r[8 * c + 2]) * inv, __uint_as_float(r[8 * c + 3]) * inv),
+                            pack_bf16x2(__uint_as_float(r[8 * c + 4]) * inv, __uint_as_float(r[8 * c + 5]) * inv),
+                            pack_bf16x2(__uint_as_float(r[8 * c + 6]) * inv, __uint_as_float(r[8 * c + 7]) * inv));
+            __syncwarp();
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              uint4 x;
-              x.x = pack_bf16x2(__uint_as_float(r[8 * c]) * inv, __uint_as_float(r[8 * c + 1]) * inv);
-              x.y = pack_bf16x2(__uint_as_float(r[8 * c + 2]) * inv, __uint_as_float(r[8 * c + 3]) * inv);
-              x.z = pack_bf16x2(__uint_as_float(r[8 * c + 4]) * inv, __uint_as_float(r[8 * c + 5]) * inv);
-              x.w = pack_bf16x2(__uint_as_float(r[8 * c + 6]) * inv, __uint_as_float(r[8 * c + 7]) * inv);
-              *reinterpret_cast<uint4*>(o + 8 * c) = x;
+              const int row = c * 8 + (lane >> 2), q = lane & 3;
+              const long long off = __shfl_sync(0xffffffffu, static_cast<long long>(n) * p.o_strides[0] + h * p.o_strides[1], row);
+              float4 x;
+              ld_shared_v4f(stage + row * 64 + ((q ^ ((row >> 1) & 3)) << 4), x.x, x.y, x.z, x.w);
+              if (warp * 32 + row < rows && ok) *reinterpret_cast<float4*>(static_cast<__nv_bfloat16*>(p.O) + off + f0 + 8 * q) = x;
             }
-          } else if (there && ok) {
+          } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-              *reinterpret_cast<float4*>(part + tid * D + f0 + 4 * c) =
-                  make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]), __uint_as_float(r[4 * c + 3]));
+            for (int c = 0; c < 8; ++c) st_shared_v4w(stage + lane * 128 + ((c ^ (lane & 7)) << 4), r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const int row = c * 4 + (lane >> 3), q = lane & 7;
+              float4 x;
+              ld_shared_v4f(stage + row * 128 + ((q ^ (row & 7)) << 4), x.x, x.y, x.z, x.w);
+              if (warp * 32 + row < rows && ok) *reinterpret_cast<float4*>(part + (warp * 32 + row) * D + f0 + 4 * q) = x;
+            }
           }
         }
       }
