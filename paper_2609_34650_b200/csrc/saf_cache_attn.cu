@@ -604,8 +604,11 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
 
 CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32, int num_sms) {
   const int rows = max_new * kv_group;
-  // (fp32 output needs weights of 24 bits, three terms of which the wide form's TMEM has no room for)
-  if (rows > 16 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len, num_sms);
+  // Units of 128 rows from 32 rows at head dimension 128, 43 at 96 and 64 at 64 on, where the two cross (us, this form / the wide one, 24 trees
+  // on up to 8192 cached tokens, head dimension 128: 20 rows 95 / 122, 32 rows 131 / 124, 64 rows 225 / 137; 64: 48 rows 56 / 67, 64 rows
+  // 70 / 67; 8 chains at 96: 32 rows 72 / 77, 48 rows 99 / 82).  fp32 output needs weights of 24 bits, three terms of which the wide
+  // form's TMEM has no room for.
+  if (rows * D >= 4096 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len, num_sms);
   CacheAttnForm f;
   f.wide = false;
   f.tile_tokens = 0;

@@ -660,7 +660,7 @@ CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, i
   f.blocks = BLOCKS * num_sms;
   f.parts = 2 * f.blocks;
   f.part_bytes = part_size(f.max_rows, D) * sizeof(float);
-  f.tiles = static_cast<int64_t>((max_new - 1) / f.tile_tokens + 1) * ((max_len - 1) / KT + 1);
+  f.tiles = static_cast<int64_t>((max_new - 1) / f.tile_tokens + 1) * ((max_len - 1) / KT + 1 + EXTRA<128>);
   return f;
 }
 

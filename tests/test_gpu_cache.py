@@ -640,3 +640,148 @@ def test_prompts_then_steps_equal_the_layer(tree):
         step += 1
     torch.cuda.synchronize()
     assert ctx.saf_last_device_status()[0] == saf.SAF_OK
+
+
+# ------------------------------------------------------------------------------------------------------------------- many rows
+@pytest.mark.parametrize("H,g,D,frozen", GEOMETRY)
+def test_many_rows_of_fp32(H, g, D, frozen):
+    Step([500, 64, 17, 333], [40, 64, 17, 3], H, g, D, 32, "slot", frozen, tree=True, out="fp32", seed=7).call_and_check()
+
+
+# frozen heads of a group: as many as have two places each, up to twice as many, and more than have one
+@pytest.mark.parametrize("nf", [1, 5, 6, 7, 12, 13, 16])
+@pytest.mark.parametrize("D,page,layout", [(64, 128, "page"), (96, 48, "slot"), (128, 16, "page")])
+@pytest.mark.parametrize("tree", [False, True])
+def test_frozen_heads_of_one_group(nf, D, page, layout, tree):
+    frozen = tuple(np.random.default_rng(nf).permutation(16)[:nf]) + tuple(16 + i for i in range(0, 16, 3))
+    Step([700, 9, 130, 65], [9, 9, 2, 1], 32, 16, D, page, layout, frozen, tree=tree, seed=nf).call_and_check()
+
+
+@pytest.mark.parametrize("H,g,D,new", [(100, 100, 64, [3, 1, 2]), (128, 128, 128, [1, 2, 1]), (130, 65, 96, [2, 3, 1]), (129, 129, 64, [2, 1, 1]), (512, 256, 64, [1, 1, 1])])
+def test_groups_of_many_heads(H, g, D, new):
+    frozen = tuple(range(0, H, 17))
+    Step([300, 3, 65], new, H, g, D, 16, "page", frozen, seed=8).call_and_check()
+
+
+@pytest.mark.parametrize("D,g", [(64, 2), (96, 4), (128, 1)])
+@pytest.mark.parametrize("ctx", [0, 1, 23, 24, 25, 63, 64, 65, 87, 88, 89])
+def test_many_rows_at_the_edges_of_tiles(D, g, ctx):
+    new = [40, 41, 39, 0, 64]
+    Step([ctx + n for n in new], new, 2 * g, g, D, 16, "page", (0,), tree=ctx % 2 == 0, seed=ctx).call_and_check()
+
+
+@pytest.mark.parametrize("D,g,frozen,page,layout", [(64, 2, (1, 2), 128, "slot"), (96, 2, (), 48, "page"), (128, 4, tuple(range(8)), 64, "slot"), (128, 2, (0, 3), 16, "page")])
+@pytest.mark.parametrize("lens", [[5000, 64, 700], [9000], [64] * 150 + [4000], [1000, 0, 2500, 64, 5999]])
+def test_many_rows_split_over_blocks(D, g, frozen, page, layout, lens):
+    new = [0 if n == 0 else 33 if i % 2 else 64 for i, n in enumerate(lens)]
+    only = range(0, len(lens), 29) if len(lens) > 100 else None
+    Step(lens, new, 2 * g, g, D, page, layout, frozen, tree=True, seed=9).call_and_check(only)
+
+
+@pytest.mark.parametrize("D,g,new", [(64, 4, 5), (64, 4, 40), (96, 2, 40), (128, 2, 6), (128, 4, 40)])
+def test_positions_anywhere(D, g, new):
+    """New tokens whose positions neither ascend nor stay near their places."""
+    s = Step([new + 300, new, new + 70], [new] * 3, 2 * g, g, D, 16, "page", (0, g), tree=True, seed=10)
+    rng = np.random.default_rng(11)
+    s.pos = [rng.integers(0, s.max_len, new) for _ in range(3)]
+    s.positions = ints([int(x) for p in s.pos for x in p] + [-9] * 2)
+    s.call_and_check()
+
+
+def test_positions_out_of_range_are_clamped():
+    for g, new in ((1, 4), (4, 40)):
+        s = Step([new + 30], [new], 2 * g, g, 128, 16, "page", (0,), tree=True, seed=12)
+        last = s.alpha.shape[1] - 1
+        s.pos = [np.array([0, last, 7, last] * (new // 4))]
+        s.positions = ints([-2 ** 31, 2 ** 31 - 1, 7, last + 1] * (new // 4) + [-9] * 2)
+        s.call_and_check()
+
+
+def test_many_rows_of_slices_scale_and_no_lse():
+    s = Step([170, 33], [33, 21], 8, 4, 128, 32, "slot", (1, 4), sliced=True, scale=0.07, positions=False)
+    s.call_and_check()
+    O = s.O.clone()
+    s.O.fill_(9.0)
+    s.call(saf.Context(0), lse=False)
+    assert torch.equal(O, s.O)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows_that_see_nothing_or_lie_out_of_range(D):
+    ctx = saf.Context(0)
+    s = Step([40, 300, 90], [40, 33, 20], 4, 2, D, frozen=(1,), tree=True, poison=0.0)
+    s.masks[1] = 0
+    s.d_lens[2] = 0
+    s.call(ctx)
+    s.check(only=[1])
+    assert not s.O[1].any() and s.O[0].any() and not s.O[73:93].any()
+    assert (s.LSE[73:93, [0, 2, 3]] == float("-inf")).all() and not s.LSE[73:93, 1].any() and (s.LSE[1, [0, 2, 3]] == float("-inf")).all()
+    # page numbers outside the pool, and offsets that do not ascend or pass N
+    s = Step([400, 140, 33], [40, 32, 33], 4, 2, D, frozen=(3,), tree=True, poison=0.0)
+    s.table[0] = torch.tensor([-1, 2 ** 31 - 1, 10 ** 6, -2 ** 31] * 10, dtype=torch.int32, device="cuda")[:s.table.shape[1]]
+    s.call(ctx)
+    s.check(only=[1, 2])
+    assert torch.isfinite(s.O).all()
+    s.d_off.copy_(ints([0, -5, 3, 10 ** 6]))
+    s.call(ctx)
+    # more rows than max_new, more tokens than max_len
+    s = Step([300, 90], [40, 34], 4, 2, D, frozen=(3,), max_new=34)
+    s.call(ctx)
+    torch.cuda.synchronize()
+    assert (s.O[34:40] == 9.0).all() and (s.O[33] != 9.0).any() and (s.O[40:74] != 9.0).any()
+    s.d_lens[1] = 1000000
+    s.call(ctx)
+    torch.cuda.synchronize()
+
+
+def test_many_rows_and_preferences_of_minus_infinity_and_of_the_lowest_value():
+    s = Step([150, 40], [33, 40], 4, 4, 64, frozen=(0, 1, 3), tree=True)
+    s.alpha[0, 10:140] = float("-inf")
+    s.alpha[1, :] = torch.finfo(torch.float32).min
+    s.alpha[1, 2] = 0.0
+    s.rho[0, 5] = float("-inf")
+    s.call_and_check()
+
+
+def test_recorded_steps_of_many_rows_on_another_stream():
+    ctx = saf.Context(0)
+    s = Step([7000, 140, 5000, 39], [33, 40, 21, 39], 8, 4, 128, frozen=(1, 2), tree=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.call(ctx)
+    s.check()
+    first = s.O.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+        s.call(ctx)
+    for _ in range(3):
+        s.O.fill_(9.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, s.O)
+    s.check()
+
+
+def test_one_context_serves_few_and_many_rows_in_turn():
+    ctx = saf.Context(0)
+    steps = [Step([900, 4000], [1, 1], 8, 2, 128, frozen=(1,)), Step([5000] * 3, [40, 1, 3], 8, 4, 128, frozen=(2,), tree=True),
+             Step([3000], [40], 4, 2, 64, out="fp32"), Step([6000, 65], [64, 64], 4, 2, 64, frozen=(0,)), Step([2], [1], 2, 1, 96)]
+    for _ in range(3):
+        for s in steps:
+            s.O.fill_(9.0), s.LSE.fill_(9.0)
+            s.call(ctx)
+        for s in steps:
+            s.check()
+
+
+def test_more_tiles_than_32_bits_are_refused():
+    s = Step([40, 3], [2, 1], 4, 2, 64, frozen=(1,))
+    for R, H, g, max_new in ((4096, 1024, 1, 16), (4096, 1024, 1, 64), (4096, 1024, 8, 64)):
+        s.prob.R, s.prob.H, s.prob.kv_group, s.prob.max_new = R, H, g, max_new
+        s.prob.page_size, s.prob.max_pages, s.prob.max_len, s.prob.Tp = 1 << 18, 1 << 8, 1 << 26, 1 << 26
+        with pytest.raises(saf.SafError) as e:
+            s.call(saf.Context(0))
+        assert e.value.code == 2
+    torch.cuda.synchronize()
