@@ -422,6 +422,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         rho_at = (KT + min(max(pos - plan.pmin, 0), 63) + KT - 1) * 4;
         any_frozen = __any_sync(0xffffffffu, frozen && there);
       }
+      const bool read = !fast || (keys && !__all_sync(0xffffffffu, frozen || !there));   // scores out of TMEM
       const float cf = frozen ? LOG2E : p.scale_log2;         // from scores to powers of two
       float m_ref = -INFINITY, l = 0.0f;
       for (int t = tb; t < te; ++t, ++count) {
@@ -431,110 +432,110 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         const uint32_t t_p = t_s + KT * (count & 1);
         if (!mbar_wait_warp_compact(&s_full[count & 1], (count >> 1) & 1, wc, SITE_S_FULL)) ok = false;
         tc_fence_after();
-        float m_new = m_ref;
+        bool waited = t == tb;                                // for the product before this one
         if (!idle) {
           if (any_frozen && !fast) slow_scores(p, w, ctx, t, h, pos, keys, frozen, t_p, newpos);
-          // 32 scores at a time, so that loads have registers to arrive in: first the maximum (what differs from the MMA's scores is
-          // written back), then the weights
-          const bool written = (any_frozen && fast) || !plain;
-          float top = -INFINITY;
+          // 16 scores at a time, in little code (32 at a time took 152 us where this takes 139, 24 trees with a third of the heads frozen: the
+          // loop over tiles has to stay in the instruction cache), and each once: the weights refer to a power of two that stays where it is until a
+          // score passes it by 2^8, and then goes 2^8 beyond the score, so that what was formed before is moved by an exact factor
+          uint64_t sum = 0;                                   // two sums
 #pragma unroll 1
-          for (int c = 0; c < KT / 32; ++c) {                 // (not unrolled: the loop over tiles has to stay in the instruction cache)
-            uint32_t r[32];
-            if (keys || !fast) {
-              tmem_ld32(t_p + 32 * c, r);
+          for (int c = 0; c < KT / 16; ++c) {
+            uint32_t r[16];
+            if (read) {
+              tmem_ld16(t_p + 16 * c, r);
               tmem_wait_ld();
             }
             if (any_frozen && fast) {
-              const uint32_t a = band_at + buf * (FZ * BAND * 4) + 128 * c;
+              const uint32_t a = band_at + buf * (FZ * BAND * 4) + 64 * c;
+              float x[16], y[16];
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
               if (plain) {
-                float x[32], y[32];
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) y[e] = ld_shared_f(a + rho_at - 256 * c - 4 * e);
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
+                for (int e = 0; e < 16; ++e) y[e] = ld_shared_f(a + rho_at - 128 * c - 4 * e);
               } else {
-                float x[32], y[32];
-                const uint32_t pl = smem_u32(places + buf * KT + 32 * c);
+                const uint32_t pl = smem_u32(places + buf * KT + 16 * c);
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                  ld_shared_v4f(a + 4 * e, x[e], x[e + 1], x[e + 2], x[e + 3]);
-                  ld_shared_v4f(pl + 4 * e, y[e], y[e + 1], y[e + 2], y[e + 3]);
-                }
+                for (int e = 0; e < 16; e += 4) ld_shared_v4f(pl + 4 * e, y[e], y[e + 1], y[e + 2], y[e + 3]);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) y[e] = ld_shared_f(a - 128 * c + rho_at - __float_as_int(y[e]));
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
+                for (int e = 0; e < 16; ++e) y[e] = ld_shared_f(a - 64 * c + rho_at - __float_as_int(y[e]));
               }
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (frozen) r[e] = __float_as_uint(x[e] + y[e]);
             }
             if (!plain) {
               // which keys the row sees
-              const int rel = ctx - (t * KT + 32 * c);
-              const uint32_t sees = rel >= 32 ? ~0u : rel > 0 ? ((1u << rel) - 1) | (static_cast<uint32_t>(mask) << rel) : rel > -64 ? static_cast<uint32_t>(mask >> -rel) : 0u;
+              const int rel = ctx - (t * KT + 16 * c);
+              const uint32_t sees = rel >= 16 ? ~0u : rel > 0 ? ((1u << rel) - 1) | (static_cast<uint32_t>(mask) << rel) : rel > -64 ? static_cast<uint32_t>(mask >> -rel) : 0u;
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
+              for (int e = 0; e < 16; ++e)
                 if (!((sees >> e) & 1)) r[e] = 0xff800000u;
             }
-            if (written) tmem_st32(t_p + 32 * c, r);
-            float mx0 = -INFINITY, mx1 = -INFINITY;
+            float top = -INFINITY, top1 = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              mx0 = max3(mx0, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-              mx1 = max3(mx1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+            for (int e = 0; e < 16; e += 4) {
+              top = max3(top, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+              top1 = max3(top1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
             }
-            top = max3(top, mx0, mx1);
+            top = fmaxf(top, top1) * cf;
+            const bool need = top - m_ref > 8.0f;             // (from -inf: always; -inf to -inf: NaN, no)
+            if (__any_sync(0xffffffffu, need)) {
+              const float to = need ? ceilf(top) + 8.0f : m_ref, d = m_ref - to;
+              const float f = !need ? 1.0f : d >= -126.0f ? __int_as_float((127 + static_cast<int>(d)) << 23) : 0.0f;
+              m_ref = to;
+              l *= f;
+              sum = mul2(sum, pk2(f, f));
+              if (!waited && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
+              waited = true;
+              tc_fence_after();
+              tmem_wait_st();
+              if (t > tb) {
+#pragma unroll 1
+                for (int cc = 0; cc < D; cc += 8) {
+                  uint32_t x[8];
+                  tmem_ld8(t_s + 128 + cc, x);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+                  tmem_st8(t_s + 128 + cc, x);
+                }
+              }
+#pragma unroll 1
+              for (int cc = 0; cc < 8 * c; cc += 8) {         // weights of this tile's first keys
+                uint32_t x[8];
+                tmem_ld8(t_p + cc, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = pack_bf16x2(__uint_as_float(x[e] << 16) * f, __uint_as_float(x[e] & 0xffff0000u) * f);
+                tmem_st8(t_p + cc, x);
+              }
+            }
+            const float neg_m = m_ref == -INFINITY ? 0.0f : -m_ref;
+            const uint64_t cf2 = pk2(cf, cf), neg2 = pk2(neg_m, neg_m);
+            uint32_t pk[8];                                   // (weights take the place of scores that have been read)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float a0, a1;
+              upk2(fma2(pk2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), cf2, neg2), a0, a1);
+              a0 = ex2_approx(a0);
+              a1 = ex2_approx(a1);
+              sum = add2(sum, pk2(a0, a1));
+              pk[e] = pack_bf16x2(a0, a1);
+            }
+            tmem_st8(t_p + 8 * c, pk);
           }
-          if (written) tmem_wait_st();
-          m_new = fmaxf(m_ref, top * cf);
+          float l0, l1;
+          upk2(sum, l0, l1);
+          l += l0 + l1;
         }
         if (fast) {                                           // (the band has been read)
           warp_arrive(&band_empty[buf]);
           if (buf) ++band1;
           else ++band0;
         }
-        if (t > tb && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
-        if (!idle) {
-          // the reference follows the maximum where that has grown by more than 2^8
-          const bool need = m_new - m_ref > 8.0f;             // (from -inf: always; -inf to -inf: NaN, no)
-          if (t == tb) {
-            m_ref = m_new;
-          } else if (__any_sync(0xffffffffu, need)) {
-            tc_fence_after();
-            const float f = need ? ex2_approx(m_ref - m_new) : 1.0f;
-            l *= f;
-            if (need) m_ref = m_new;
-#pragma unroll 1
-            for (int cc = 0; cc < D / 16; ++cc) {
-              uint32_t x[16];
-              tmem_ld16(t_s + 128 + 16 * cc, x);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-              tmem_st16(t_s + 128 + 16 * cc, x);
-            }
-          }
-          const float neg_m = m_ref == -INFINITY ? 0.0f : -m_ref;
-          float sum[2] = {0.0f, 0.0f};
-#pragma unroll 1
-          for (int c = 0; c < KT / 32; ++c) {                 // (the weights of 32 keys take the place of scores that have been read)
-            uint32_t r[32], pk[16];
-            tmem_ld32(t_p + 32 * c, r);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float a0 = ex2_approx(fmaf(__uint_as_float(r[2 * e]), cf, neg_m)), a1 = ex2_approx(fmaf(__uint_as_float(r[2 * e + 1]), cf, neg_m));
-              sum[0] += a0;
-              sum[1] += a1;
-              pk[e] = pack_bf16x2(a0, a1);
-            }
-            tmem_st16(t_p + 16 * c, pk);
-          }
-          l += sum[0] + sum[1];
-        }
+        if (!waited && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;   // (each phase is waited for in turn)
         if (!plain) {
           if (!mbar_wait_warp_compact(&v_full[count % C::ST], (count / C::ST) & 1, wc, SITE_V_FULL)) ok = false;
           if (clean_values<D>(p.box_rows, t * KT, ctx, w.len, smem_u32(smem) + C::OFF_V + (count % C::ST) * C::TILE, tid)) wild_s = 1;
