@@ -361,7 +361,8 @@ int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, cons
  *   ordinary head that sees nothing
  * Q rows of frozen heads are never read, nor keys where all heads of a group are frozen.  D in {64, 96, 128}; R * (H / kv_group) *
  * ceil(max_len / 16) * ceil(max_new * kv_group / 8) < 2^31 (SAF_ERR_UNSUPPORTED beyond what the kernels' tiles reach, which is no less).
- * Results do not vary from run to run.  One launch; recordable after one warm-up call with the same kv_group, D, max_new and o_dtype. */
+ * Results do not vary from run to run.  One launch; recordable after one warm-up call with the same kv_group, D, max_new and o_dtype, and
+ * recorded calls stay good when calls of other sizes follow in the context. */
 int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* k_cache, const void* v_cache,
                    const int32_t* block_table, const int32_t* new_offsets, const int32_t* kv_lens, const int32_t* positions,
                    const uint64_t* tree_masks, const uint8_t* frozen_mask_host, const float* alpha, const float* rho, void* O,

@@ -1693,7 +1693,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
     return SAF_ERR_INVALID_ARG;
   const int kvg = c->kv_group > 1 ? c->kv_group : 1;
   // (tiles are counted in 32 bits)
-  const CacheAttnForm form = cache_attn_form(c->max_new, kvg, c->D, c->page_size, c->max_len, c->o_dtype == SAF_F32, ctx->num_sms);
+  const CacheAttnForm form = cache_attn_form(c->max_new, kvg, c->D, c->page_size, c->max_len, c->o_dtype == SAF_F32);
   if (form.tiles > 0x7fffffffLL / (static_cast<int64_t>(c->R) * (c->H / kvg))) return SAF_ERR_UNSUPPORTED;
   CacheAttnParams f{};
   int nf = 0;
@@ -1737,7 +1737,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.box_rows = form.box_rows;
   f.v = v_cache;
   for (int i = 0; i < 3; ++i) f.v_strides[i] = c->v_strides[i];
-  if ((rc = ensure(ctx->cattn_buf, form.parts * form.part_bytes)) || (rc = ensure(ctx->cattn_counters, form.blocks * sizeof(int))) ||
+  if ((rc = ensure(ctx->cattn_buf, cache_attn_workspace(ctx->num_sms))) || (rc = ensure(ctx->cattn_counters, CACHE_BLOCKS * ctx->num_sms * sizeof(int))) ||
       (rc = zero_if_fresh(ctx->cattn_counters, st)))
     return rc;
   f.workspace = static_cast<float*>(ctx->cattn_buf.ptr);

@@ -602,25 +602,27 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams
 
 }  // namespace
 
-CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32, int num_sms) {
+CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32) {
   const int rows = max_new * kv_group;
   // Units of 128 rows from 32 rows at head dimension 128, 43 at 96 and 64 at 64 on, where the two cross (us, this form / the wide one, 24 trees
   // on up to 8192 cached tokens, head dimension 128: 20 rows 95 / 122, 32 rows 131 / 124, 64 rows 225 / 137; 64: 48 rows 56 / 67, 64 rows
   // 70 / 67; 8 chains at 96: 32 rows 72 / 77, 48 rows 99 / 82).  fp32 output needs weights of 24 bits, three terms of which the wide
   // form's TMEM has no room for.
-  if (rows * D >= 4096 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len, num_sms);
+  if (rows * D >= 4096 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len);
   CacheAttnForm f;
   f.wide = false;
   f.tile_tokens = 0;
   f.max_rows = std::min(16, rows);
   f.halves_k = f.halves_v = D == 128 ? 2 : 1;
   f.box_rows = D == 64 && page_size % 32 == 0 ? 32 : 16;
-  f.blocks = num_sms;
-  f.parts = num_sms * (2 + Cfg<64, 1>::WARPS);
-  f.part_bytes = part_size(f.max_rows, D) * sizeof(float);
   const int unit = rows <= 8 ? 8 : 16, keys = D == 64 ? 32 : 16;
   f.tiles = static_cast<int64_t>((rows - 1) / unit + 1) * ((max_len - 1) / keys + 1);
   return f;
+}
+
+// (two parts a block, and one a warp where shared memory has no room for them)
+size_t cache_attn_workspace(int num_sms) {
+  return std::max(sizeof(float) * (2 + Cfg<64, 1>::WARPS) * num_sms * part_size(16, 128), cache_wide_workspace(num_sms));
 }
 
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st) {

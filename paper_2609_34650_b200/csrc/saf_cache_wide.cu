@@ -20,7 +20,7 @@ namespace {
 
 constexpr int ROWS = 128, KT = 64, W = 8, NT = 32 * W, FZ = 6, BAND = 256;
 constexpr int SINGLE_TILES = 16;    // tiles up to which a block takes a whole unit where there are no more units than blocks
-constexpr int BLOCKS = 2;           // blocks an SM
+constexpr int BLOCKS = CACHE_BLOCKS;
 
 template <int D>
 struct Cfg {
@@ -649,7 +649,7 @@ cudaError_t launch(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttn
 
 }  // namespace
 
-CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, int max_len, int num_sms) {
+CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, int max_len) {
   CacheAttnForm f;
   f.wide = true;
   f.tile_tokens = ROWS / kv_group;
@@ -658,12 +658,11 @@ CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, i
   f.halves_v = D == 128 ? 2 : 1;
   f.box_rows = 16;
   while (f.box_rows < KT && page_size % (2 * f.box_rows) == 0) f.box_rows *= 2;
-  f.blocks = BLOCKS * num_sms;
-  f.parts = 2 * f.blocks;
-  f.part_bytes = part_size(f.max_rows, D) * sizeof(float);
   f.tiles = static_cast<int64_t>((max_new - 1) / f.tile_tokens + 1) * ((max_len - 1) / KT + 1 + EXTRA<128>);
   return f;
 }
+
+size_t cache_wide_workspace(int num_sms) { return sizeof(float) * 2 * BLOCKS * num_sms * part_size(ROWS, 128); }
 
 cudaError_t launch_cache_wide(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnParams& p, int num_sms, cudaStream_t st) {
   if (p.D == 64) return launch<64>(mk, mv, p, num_sms, st);

@@ -348,12 +348,15 @@ struct CacheAttnForm {
   int tile_tokens;                  // wide: new tokens of a unit
   int max_rows;                     // rows of a unit's part
   int halves_k, halves_v, box_rows; // of the pools' tensor maps: [pages][heads][feature halves][slots][features], boxes of box_rows slots x 64 features
-  int blocks, parts;                // counters, and parts in the workspace
-  size_t part_bytes;
   int64_t tiles;                    // of a request of the bounds' size, a cached head
 };
-CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32, int num_sms);
-CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, int max_len, int num_sms);
+CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, int max_len, bool o_f32);
+CacheAttnForm cache_wide_form(int max_new, int kv_group, int D, int page_size, int max_len);
+// Bytes of the parts that any call may leave between its blocks, and counters of blocks: of one size for all calls, so that a recorded call's
+// workspace stays where it is when larger ones follow (39 MB on 148 SMs).
+size_t cache_attn_workspace(int num_sms);
+size_t cache_wide_workspace(int num_sms);
+constexpr int CACHE_BLOCKS = 2;            // blocks an SM at most
 cudaError_t launch_cache_attn(const CUtensorMap& mk, const CUtensorMap& mv, CacheAttnParams& p, int num_sms, cudaStream_t st);
 cudaError_t launch_cache_wide(const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnParams& p, int num_sms, cudaStream_t st);
 

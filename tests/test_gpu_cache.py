@@ -785,3 +785,22 @@ def test_more_tiles_than_32_bits_are_refused():
             s.call(saf.Context(0))
         assert e.value.code == 2
     torch.cuda.synchronize()
+
+
+def test_recorded_step_after_a_larger_call():
+    """The workspace of a recorded call stays where it is when calls with more rows and wider heads follow."""
+    ctx = saf.Context(0)
+    s = Step([4000, 300, 77], [1, 1, 1], 8, 2, 64, frozen=(1,))
+    s.call(ctx)
+    s.check()
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+        s.call(ctx)
+    for other in (Step([5000], [40], 4, 2, 128, out="fp32"), Step([3000, 400], [64, 33], 8, 4, 128, frozen=(2,), tree=True)):
+        other.call(ctx)
+        other.check()
+        s.O.fill_(9.0), s.LSE.fill_(9.0)
+        torch.cuda.synchronize()
+        g.replay()
+        s.check()
