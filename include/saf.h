@@ -359,7 +359,7 @@ int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, cons
  *   frozen_mask_host, alpha, rho as in saf_hybrid_attn_fwd (no logZ: the sum over the keys is formed here); H <= 1024
  *   LSE: device fp32 [N][H] or NULL: natural-log sum of exp of the scaled scores, 0 for frozen heads, -inf for a row of an
  *   ordinary head that sees nothing
- * Q rows of frozen heads are never read, nor keys where all heads of a group are frozen.  D in {64, 96, 128}; R * (H / kv_group) *
+ * Q rows of frozen heads are never read, nor keys where all heads of a group are frozen.  D in {64, 96, 128}; max_len <= 2^31 - 256; R * (H / kv_group) *
  * ceil(max_len / 16) * ceil(max_new * kv_group / 8) < 2^31 (SAF_ERR_UNSUPPORTED beyond what the kernels' tiles reach, which is no less).
  * Results do not vary from run to run.  One launch; recordable after one warm-up call with the same kv_group, D, max_new and o_dtype, and
  * recorded calls stay good when calls of other sizes follow in the context. */

@@ -218,6 +218,7 @@ def make_rotary(q, k, q_out, k_out, rot_dim, interleaved=False, mscale=1.0):
             continue
         assert t.stride(-1) == 1, "feature stride must be 1"
         assert t.shape == like.shape and t.shape[-1] == r.D and t.dim() == first.dim(), "outputs have their inputs' shapes"
+        assert t.shape[0] == first.shape[0] and (packed or t.shape[2] == r.T), "queries and keys have the same tokens"
         assert _dtype(t) == (r.in_dtype if name[1] == "_" else r.out_dtype), "one dtype for both inputs, one for both outputs"
         arr = getattr(r, name)
         arr[0], arr[1], arr[2] = (t.shape[0] * t.stride(0), t.stride(1), t.stride(0)) if packed else (t.stride(0), t.stride(1), t.stride(2))
@@ -241,10 +242,16 @@ def make_cache(R, N, page_size, n_pages, max_pages, k_cache=None, v_cache=None, 
         if t is not None:
             assert t.stride(2) == 1 and t.shape[0] == N and t.shape[2] == c.D, "packed rows are [N,heads,D]"
             getattr(c, name)[:] = [t.stride(0), t.stride(1)]
+    if k_cache is not None and v_cache is not None:
+        assert k_cache.shape == v_cache.shape, "one shape of both pools"
+    if v_like is not None:
+        assert v_like.shape[1] == c.H, "new values have the pools' heads"
     if q_like is not None:
+        assert q_like.shape[1] % c.H == 0, "query heads are a multiple of the pools' heads"
         c.kv_group = q_like.shape[1] // c.H
         c.H = q_like.shape[1]
     if o_like is not None:
+        assert o_like.shape[1] == c.H, "outputs have the query heads"
         c.o_dtype = _dtype(o_like)
     return c
 

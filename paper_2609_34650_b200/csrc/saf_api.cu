@@ -1685,7 +1685,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   if (!ctx) return SAF_ERR_INVALID_ARG;
   int rc = validate_cache(c);
   if (rc || (rc = validate_pools(c))) return rc;
-  if ((c->D != 64 && c->D != 96 && c->D != 128) || c->page_size % 16 != 0 || c->H > CACHE_MAX_HEADS ||
+  if ((c->D != 64 && c->D != 96 && c->D != 128) || c->page_size % 16 != 0 || c->H > CACHE_MAX_HEADS || c->max_len > 0x7fffff00 ||
       (c->o_dtype != SAF_F32 && c->o_dtype != SAF_BF16))
     return SAF_ERR_UNSUPPORTED;
   if (!frozen_mask_host || c->max_new < 1 || c->max_new > 64 || c->max_len < 1 ||

@@ -120,3 +120,24 @@ def test_struct_layout_matches_header(tmp_path, name, cls, words):
     out = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     assert out == [ctypes.sizeof(cls)] + [getattr(cls, f).offset for f in fields]
     assert getattr(cls, "q_strides").offset == 4 * words
+
+
+def test_make_cache_refuses_arrays_that_do_not_fit_together():
+    torch = pytest.importorskip("torch")
+    kc = torch.zeros((5, 3, 16, 64), dtype=torch.bfloat16)
+    q = torch.zeros((7, 6, 64), dtype=torch.bfloat16)
+    c = saf.make_cache(2, 7, 16, 5, 4, k_cache=kc, v_cache=kc, q_like=q, o_like=q, v_like=q[:, :3])
+    assert (c.H, c.kv_group, c.D, c.o_dtype) == (6, 2, 64, 0)
+    for change in (dict(q_like=q[:, :4]), dict(o_like=q[:, :3]), dict(v_like=q), dict(v_cache=kc[:, :2]), dict(k_cache=kc[:4]), dict(q_like=q[:5])):
+        with pytest.raises(AssertionError):
+            saf.make_cache(2, 7, 16, 5, 4, **dict(dict(k_cache=kc, v_cache=kc, q_like=q, o_like=q, v_like=q[:, :3]), **change))
+
+
+def test_make_rotary_refuses_arrays_that_do_not_fit_together():
+    torch = pytest.importorskip("torch")
+    q, k = torch.zeros((2, 4, 9, 64)), torch.zeros((2, 2, 9, 64))
+    r = saf.make_rotary(q, k, q, k, 64)
+    assert (r.B, r.T, r.Hq, r.Hk, r.D) == (2, 9, 4, 2, 64)
+    for args in ((q, k[:, :, :8], q, k[:, :, :8]), (q, k[:1], q, k[:1]), (q, k, q[:, :3], k), (q, k, q, k.bfloat16()), (q, k[0], q, k[0])):
+        with pytest.raises(AssertionError):
+            saf.make_rotary(*args, 64)

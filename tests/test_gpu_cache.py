@@ -784,6 +784,11 @@ def test_more_tiles_than_32_bits_are_refused():
         with pytest.raises(saf.SafError) as e:
             s.call(saf.Context(0))
         assert e.value.code == 2
+    s.prob.R = s.prob.H = s.prob.kv_group = s.prob.max_new = 1           # lengths whose tiles would end beyond 2^31
+    s.prob.max_pages, s.prob.page_size, s.prob.max_len = 2 ** 24 - 1, 128, 2 ** 31 - 128
+    with pytest.raises(saf.SafError) as e:
+        s.call(saf.Context(0))
+    assert e.value.code == 2
     torch.cuda.synchronize()
 
 
