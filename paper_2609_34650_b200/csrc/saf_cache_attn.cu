@@ -12,6 +12,8 @@
 // The products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that keys and features fill the 16-row side of the matrix
 // instructions and the few rows of a step their 8-column side (with rows on the 16-row side the kernel issued twice the
 // instructions, which bound it at 550 a tile of 16 keys).
+// 16 requests of up to 32768 tokens, 32 heads on 8 of 128: 187 us = 5.9 TB/s, 90 % of a large copy's rate.  32 requests of up to 4096, 12 heads of 64:
+// 45 us = 4.0 TB/s, of which 8 us pass before the first tile and 9 in the joins.
 #include "saf_cache_attn.cuh"
 
 namespace saf {
