@@ -809,3 +809,30 @@ def test_recorded_step_after_a_larger_call():
         torch.cuda.synchronize()
         g.replay()
         s.check()
+
+
+def test_two_contexts_of_many_rows_on_two_streams():
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    steps = [Step([4000, 300, 77], [40, 33, 64], 8, 4, 128, frozen=(1,), tree=True, seed=i) for i in range(2)]
+    ctxs = [saf.Context(0) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, s, c in zip(streams, steps, ctxs):
+            with torch.cuda.stream(st):
+                s.call(c)
+    for s in steps:
+        s.check()
+
+
+@pytest.mark.parametrize("D,g,new,out", [(64, 2, 1, "bf16"), (128, 4, 3, "fp32"), (128, 4, 40, "bf16")])
+def test_the_same_call_twice_gives_the_same_bits(D, g, new, out):
+    ctx = saf.Context(0)
+    s = Step([9000, 1200, 65], [new] * 3, 2 * g, g, D, 16, "page", (0,), tree=True, out=out, seed=13)
+    s.call(ctx)
+    torch.cuda.synchronize()
+    O, L = s.O.clone(), s.LSE.clone()
+    for c in (ctx, saf.Context(0)) * 5:
+        s.O.fill_(9.0), s.LSE.fill_(9.0)
+        s.call(c)
+        torch.cuda.synchronize()
+        assert torch.equal(O, s.O) and torch.equal(L, s.LSE)
