@@ -12,7 +12,7 @@
 // take 12 a tile), warp 6 issues the MMAs and owns TMEM, warp 7 fetches bands.  TMEM columns [0,64) and [64,128) S (fp32) of even and odd tiles, then their
 // weights (bf16 pairs) in the first half of each, [128,256) O.  Frozen rows replace their scores by alpha + rho out of a band that is
 // copied in ahead: 64 preferences of keys and 192 of distances for each of up to FZ frozen heads (up to twice as many
-// in one place instead of two); with more of them, or positions far apart, they take them from global memory.
+// in one place instead of two); with more of them, or positions that are not near the tokens' places, they take them from global memory.
 //
 // 24 trees of up to 32 tokens on up to 8192 cached ones, 32 heads on 8, a third of them frozen: 135 us = 3.1 TB/s, 107 us without frozen
 // heads.  In the second a tile and block takes 2740 clk, DRAM's rate for two blocks; the rest is the units' ends (12000 clk until the first
@@ -103,12 +103,15 @@ __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint
   return wild;
 }
 
-// Whether and how a unit's frozen rows go by bands; by a whole warp, the same for all.
+// Whether and how a unit's frozen rows go by bands; by a whole warp, the same for all.  A band serves a row whose position is at most 63 past the
+// unit's first, and a key whose position is at most 63 from its tile's first slot: a cached key's is its place; a new token's, whichever of the
+// request's it is, has to lie between the first new place and its own, as positions by place or by depth do.  (Out of line, once for both kinds of warps that ask: 24 trees 137 us, 141
+inlined.)
 struct BandPlan {
   int n_frozen, pmin, span;
   bool fast, ahead;                 // by bands; in two places in turn
 };
-__device__ __forceinline__ BandPlan plan_band(const CacheAttnParams& p, const Unit& w) {
+__device__ __noinline__ BandPlan plan_band(const CacheAttnParams& p, const Unit& w) {
   BandPlan b{0, 0, 0, false, false};
   for (int c = 0; c < p.kv_group; ++c) {
     const int hk = w.hk * p.kv_group + c;
@@ -117,14 +120,20 @@ __device__ __forceinline__ BandPlan plan_band(const CacheAttnParams& p, const Un
   if (b.n_frozen == 0) return b;
   const int ctx = w.len - w.many, t0 = w.rt * p.tile_tokens, t1 = min(t0 + p.tile_tokens, w.many);
   int lo = 0x7fffffff, hi = 0;
-  for (int c = t0 + (threadIdx.x & 31); c < t1; c += 32) {
+  bool near = ctx >= 0;
+#pragma unroll
+  for (int c = threadIdx.x & 31; c < 64; c += 32) {
+    if (c >= w.many) continue;
     const int x = p.positions ? min(max(p.positions[w.first + c], 0), p.Tp - 1) : max(ctx + c, 0);
-    lo = min(lo, x);
-    hi = max(hi, x);
+    near &= x >= ctx && x <= ctx + c;
+    if (c >= t0 && c < t1) {
+      lo = min(lo, x);
+      hi = max(hi, x);
+    }
   }
   b.pmin = __reduce_min_sync(0xffffffffu, lo);
   b.span = __reduce_max_sync(0xffffffffu, hi) - b.pmin;
-  b.fast = b.n_frozen <= 2 * FZ && b.pmin >= ctx && b.span < 64 && ctx >= 0;
+  b.fast = b.n_frozen <= 2 * FZ && b.span < 64 && __all_sync(0xffffffffu, near);
   b.ahead = b.fast && b.n_frozen <= FZ;
   return b;
 }
@@ -323,9 +332,9 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
       const int tb = tile_at(u, x0), te = tile_at(u, x1);
       if (tb >= te) continue;
+      const int ctx = u.len - u.many;
       const BandPlan b = plan_band(p, u);
       if (!b.fast) continue;
-      const int ctx = u.len - u.many;
       for (int s = 0; s < 2 && ok; ++s) ok = mbar_wait_warp_compact(&band_empty[s], (used[s] & 1) ^ 1, wc, SITE_BAND_EMPTY);
       for (int t = tb; t < te && ok; ++t) {
         const int buf = b.ahead ? (t - tb) & 1 : 0, j0 = t * KT;
@@ -337,7 +346,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         for (int i = 0; i < 2; ++i) {
           const int y = lane + 32 * i, j = j0 + y;
           at[i] = j < ctx ? j : j >= u.len ? -1 : p.positions ? min(max(p.positions[u.first + j - ctx], 0), p.Tp - 1) : j;
-          if (j0 + KT > ctx) places[buf * KT + y] = 4 * min(max(at[i] < 0 ? y : at[i] - j0, -63), KT - 1);   // (new tokens lie at their positions)
+          if (j0 + KT > ctx) places[buf * KT + y] = 4 * (at[i] < 0 ? y : at[i] - j0);   // (new tokens lie at their positions)
         }
         uint32_t dst = smem_u32(bands + buf * FZ * BAND + lane);
         const int d0 = b.pmin - j0 - (KT - 1) + lane;
