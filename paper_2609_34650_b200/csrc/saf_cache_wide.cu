@@ -106,7 +106,7 @@ __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint
 // Whether and how a unit's frozen rows go by bands; by a whole warp, the same for all.  A band serves a row whose position is at most 63 past the
 // unit's first, and a key whose position is at most 63 from its tile's first slot: a cached key's is its place; a new token's, whichever of the
 // request's it is, has to lie between the first new place and its own, as positions by place or by depth do.  (Out of line, once for both kinds of warps that ask: 24 trees 137 us, 141
-inlined.)
+// inlined.)
 struct BandPlan {
   int n_frozen, pmin, span;
   bool fast, ahead;                 // by bands; in two places in turn
