@@ -424,7 +424,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       int pos = 0;
       if (plan.n_frozen > 0) {
         pos = newpos[i];
-        if (frozen && p.positions) {                         // (new tokens behind the row's position are not seen)
+        if (frozen && (p.positions || p.masks)) {            // (new tokens behind the row's position are not seen)
           for (int c = 0; c < w.many; ++c)
             if (newpos[c] > pos) mask &= ~(1ull << c);
         }

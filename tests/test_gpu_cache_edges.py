@@ -43,3 +43,16 @@ def test_row_tiles_of_one_request_at_positions_far_apart(D, out, tree):
     third[8:24] = np.arange(16) * 3
     place(s, [first, second, third])
     s.call_and_check()
+
+
+@pytest.mark.parametrize("g,D,new", [(4, 64, 9), (4, 64, 40), (2, 96, 40), (1, 128, 9), (4, 128, 64)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_sets_with_later_tokens_and_no_positions(g, D, new, out):
+    """Positions left out are the tokens' places, so a frozen row drops the later tokens of its set and an ordinary row sees them."""
+    s = Step([200 + new, new, 65 + new], [new] * 3, 2 * g, g, D, 16, "page", (0, 2 * g - 1), out=out, tree=True, seed=new)
+    rng = np.random.default_rng(new)
+    s.sets = [[int(x) for x in rng.integers(0, 2 ** 63, new, dtype=np.uint64) & np.uint64((1 << new) - 1)] for _ in range(3)]
+    s.masks = torch.from_numpy(np.array([x for t in s.sets for x in t] + [0] * 2, dtype=np.uint64).view(np.int64)).cuda()
+    s.pos = [n - new + np.arange(new) for n in s.lens]
+    s.positions = None
+    s.call_and_check()
