@@ -352,7 +352,8 @@ int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, cons
  *   frozen head     O = sum_j w_j V_j / sum_j w_j over the keys seen, w_j = exp(alpha[h][p_j] + rho[h][p - p_j]), p_j = j for j < ctx and
  *                   the new token's position otherwise, p the row's own (keys with p_j > p count as not seen).  Where the keys seen hold each position
  *                   0..p once (a chain; a tree's ancestors), that is P^ V of Eq. "compact-prior" with its own Z(p).
- * A row that sees nothing gives zeros.  NaN and infinities in slots that a row does not see do not reach it.
+ *                   Finite preferences count whatever their size; a key whose alpha + rho, a sum in fp32, is -inf has no weight.
+ * A row that sees nothing, or nothing with weight, gives zeros.  NaN and infinities in slots that a row does not see do not reach it.
  *   Q, O: [N][H][D] by c->q_strides, o_strides; K and V pools; block_table, new_offsets, kv_lens as from saf_cache_plan (lengths beyond
  *   max_len and page numbers outside the pool are clamped, rows beyond max_new of a request are left as they are)
  *   positions [N] of the new tokens, or NULL: ctx + place (read for frozen heads only; values outside [0, Tp) are clamped)

@@ -1721,7 +1721,7 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
     if (c->page_size == 16 << b) f.page_shift = b;
   f.page_size = c->page_size; f.n_pages = c->n_pages; f.max_pages = c->max_pages;
   f.max_len = c->max_len; f.max_new = c->max_new;
-  f.scale_log2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * 1.4426950408889634f;
+  f.scale_log16 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt(static_cast<float>(c->D))) * (1.4426950408889634f / 4);
   f.q = Q;
   for (int i = 0; i < 2; ++i) {
     f.q_strides[i] = c->q_strides[i];

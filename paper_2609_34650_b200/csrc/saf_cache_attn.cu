@@ -1,7 +1,7 @@
 // Attention of a step's new tokens over a paged cache, ordinary and frozen heads side by side.
 //
 //   O_i = sum_j e^{s_ij} V_j / sum_j e^{s_ij} over the keys j that row i sees; s_ij = scale q_i k_j (ordinary head) or
-//   alpha(p_j) + rho(p_i - p_j) (frozen head), running maximum and sum in fp32, in powers of two.
+//   alpha(p_j) + rho(p_i - p_j) (frozen head), running maximum and sum in fp32, in powers of 16.
 //
 // Every key and value is read once for all rows that share it, so DRAM bounds the call unless it is a short one.  A unit is one request,
 // one cached head and up to 8 or 16 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
@@ -311,13 +311,13 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
 #pragma unroll
           for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[b][sub][e] = (SUB == 1 ? s[b][sub][e] + s2[b][e] : s[b][sub][e]) * p.scale_log2;
+            for (int e = 0; e < 4; ++e) s[b][sub][e] = __fmul_rn(SUB == 1 ? s[b][sub][e] + s2[b][e] : s[b][sub][e], p.scale_log16);
       }
       if (any_frozen) {
 #pragma unroll
         for (int x = 0; x < NP; ++x) {
           const int b = x / (SUB * 4), sub = x / 4 % SUB;
-          if (frozen[b][x & 1]) s[b][sub][x & 3] = (fa[x] + fr[x]) * LOG2E;
+          if (frozen[b][x & 1]) s[b][sub][x & 3] = __fmul_rn(fa[x] + fr[x], LOG16E);
         }
         if (t + 1 < t_end) prefer(t + 1);
       }
@@ -354,7 +354,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float c = x == -INFINITY ? 1.0f : ex2_approx(m[b][e] - x);
+            const float c = x == -INFINITY ? 1.0f : ex16(m[b][e] - x);
             m[b][e] = x;
             l[b][e] *= c;
 #pragma unroll
@@ -373,7 +373,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const float x = ex2_approx(s[b][sub][2 * half + e] - base);
+              const float x = ex16(__fsub_rn(s[b][sub][2 * half + e], base));   // (rounded scores: alike ones differ by nothing)
               s[b][sub][2 * half + e] = x;
               l[b][e] += x;
             }
@@ -505,7 +505,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         }
         if (row < rows && gid < 2 && p.LSE) {
           const bool fz = (p.frozen[h >> 5] >> (h & 31)) & 1;
-          p.LSE[static_cast<int64_t>(n) * p.H + h] = fz ? 0.0f : ls == 0.0f ? -INFINITY : (ms + log2f(ls)) * LN2;
+          p.LSE[static_cast<int64_t>(n) * p.H + h] = fz ? 0.0f : ls == 0.0f ? -INFINITY : natural_lse(ms, ls);
         }
       }
     } else {

@@ -10,7 +10,11 @@
 namespace saf {
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// Scores, maxima and references are kept in powers of 16: log16(e) is below one, so that every finite fp32 score stays finite (alpha + rho of keys
+// that mask may be the type's lowest value), and a score in powers of two is four times as many, without rounding.
+constexpr float LOG16E = 1.4426950408889634f / 4, LN2 = 0.6931471805599453f;
+__device__ __forceinline__ float ex16(float x) { return ex2_approx(4.0f * x); }
+__device__ __forceinline__ float natural_lse(float m, float l) { return fmaf(m, 4.0f * LN2, log2f(l) * LN2); }
 
 // Where a run stands: a unit, and its place on the line of all tiles.
 struct Unit {
@@ -109,7 +113,7 @@ __device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part& 
   }
   if (f == 0 && p.LSE) {
     const bool frozen = (p.frozen[h >> 5] >> (h & 31)) & 1;
-    p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
+    p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : natural_lse(m, l);
   }
 }
 
@@ -156,13 +160,13 @@ __device__ __forceinline__ void join(const CacheAttnParams& p, const Part& u, in
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, ms[k][i]);
         const float base = top == -INFINITY ? 0.0f : top;
-        const float c = ex2_approx(m[k] - base);
+        const float c = ex16(m[k] - base);
         m[k] = top;
         l[k] *= c;
         x[k].x *= c; x[k].y *= c; x[k].z *= c; x[k].w *= c;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-          const float w = ex2_approx(ms[k][i] - base);       // (absent: 0, of zeros)
+          const float w = ex16(ms[k][i] - base);             // (absent: 0, of zeros)
           l[k] += w * ls[k][i];
           x[k].x += w * v[k][i].x; x[k].y += w * v[k][i].y; x[k].z += w * v[k][i].z; x[k].w += w * v[k][i].w;
         }

@@ -436,8 +436,10 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         any_frozen = __any_sync(0xffffffffu, frozen && there);
       }
       const bool read = !fast || (keys && !__all_sync(0xffffffffu, frozen || !there));   // scores out of TMEM
-      const float cf = frozen ? LOG2E : p.scale_log2;         // from scores to powers of two
+      const float cf = frozen ? LOG16E : p.scale_log16;       // from scores to powers of 16
       float m_ref = -INFINITY, l = 0.0f;
+      float factor = cf, offset = 0.0f;                       // a weight is 2^(factor score + offset); to begin with, finite for finite scores
+      float limit = -INFINITY;                                // of that exponent, beyond which the reference moves
       for (int t = tb; t < te; ++t, ++count) {
         const bool plain = (t + 1) * KT <= ctx;               // all of its keys were cached before the step
         const int buf = plan.ahead ? (t - tb) & 1 : 0;
@@ -449,8 +451,11 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         if (!idle) {
           if (any_frozen && !fast) slow_scores(p, w, ctx, t, h, pos, keys, frozen, t_p, newpos);
           // 16 scores at a time, in little code (32 at a time took 152 us where this takes 139, 24 trees with a third of the heads frozen: the
-          // loop over tiles has to stay in the instruction cache), and each once: the weights refer to a power of two that stays where it is until a
-          // score passes it by 2^8, and then goes 2^8 beyond the score, so that what was formed before is moved by an exact factor
+          // loop over tiles has to stay in the instruction cache), and each once: the weights refer to a power of 16 that stays where it is until a
+          // score passes it by 2^8, and then goes 2^8 to 2^12 beyond the score, so that what was formed before is moved by an exact factor.
+          // From 2^27 powers of 16 on, either way, the next smaller score counts for nothing, but rounding the reference moves it by powers of two
+          // (keys masked by a low value, when a row sees no others yet): there the reference is the score as it came, and only
+          // scores that equal it have weight.
           uint64_t sum = 0;                                   // two sums
 #pragma unroll 1
           for (int c = 0; c < KT / 16; ++c) {
@@ -492,12 +497,19 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               top = max3(top, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
               top1 = max3(top1, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
             }
-            top = fmaxf(top, top1) * cf;
-            const bool need = top - m_ref > 8.0f;             // (from -inf: always; -inf to -inf: NaN, no)
+            top = fmaxf(top, top1);
+            const bool need = fmaf(top, factor, offset) > limit;
             if (__any_sync(0xffffffffu, need)) {
-              const float to = need ? ceilf(top) + 8.0f : m_ref, d = m_ref - to;
-              const float f = !need ? 1.0f : d >= -126.0f ? __int_as_float((127 + static_cast<int>(d)) << 23) : 0.0f;
-              m_ref = to;
+              const float at = __fmul_rn(top, cf);
+              const bool far = fabsf(at) >= 134217728.0f;
+              const float to = far ? at : ceilf(at) + 2.0f, d = 4.0f * (m_ref - to);
+              const float f = !need ? 1.0f : !far && d >= -126.0f ? __int_as_float((127 + static_cast<int>(d)) << 23) : 0.0f;
+              if (need) {
+                m_ref = to;
+                factor = far ? __int_as_float(__float_as_int(4.0f * cf) & 0x7f800000) : 4.0f * cf;   // (a power of two: no rounding)
+                offset = -(far ? top * factor : 4.0f * to);
+                limit = 8.0f;
+              }
               l *= f;
               sum = mul2(sum, pk2(f, f));
               if (!waited && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;
@@ -525,8 +537,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
                 tmem_st8(t_p + cc, x);
               }
             }
-            const float neg_m = m_ref == -INFINITY ? 0.0f : -m_ref;
-            const uint64_t cf2 = pk2(cf, cf), neg2 = pk2(neg_m, neg_m);
+            const uint64_t cf2 = pk2(factor, factor), neg2 = pk2(offset, offset);
             uint32_t pk[8];                                   // (weights take the place of scores that have been read)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -621,7 +632,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           part[p.max_rows * D + tid] = m_ref;
           part[p.max_rows * (D + 1) + tid] = l;
         } else if (p.LSE) {
-          p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : (m_ref + log2f(l)) * LN2;
+          p.LSE[static_cast<int64_t>(n) * p.H + h] = frozen ? 0.0f : l == 0.0f ? -INFINITY : natural_lse(m_ref, l);
         }
       }
       if (!whole && tid == 0) open_unit[x0 >= w.start ? 0 : 1] = Part{w.start, w.start + w.tiles - 1, w.first, w.many, w.rt, w.hk};

@@ -324,7 +324,7 @@ struct CacheAttnParams {
   uint32_t group_magic;             // ceil(2^32 / kv_group)
   int page_shift;                   // log2(page_size / 16), -1 if that is no power of two
   int page_size, n_pages, max_pages, max_len, max_new;
-  float scale_log2;
+  float scale_log16;                // from products of queries and keys to scores in powers of 16
   const void* q; const void* v;     // (the pools are read through their maps, but for a few values)
   int64_t q_strides[2], o_strides[2], v_strides[3];
   const int* block_table; const int* new_offsets; const int* kv_lens; const int* positions;

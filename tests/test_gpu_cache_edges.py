@@ -56,3 +56,107 @@ def test_sets_with_later_tokens_and_no_positions(g, D, new, out):
     s.pos = [n - new + np.arange(new) for n in s.lens]
     s.positions = None
     s.call_and_check()
+
+
+# ------------------------------------------------------------------------------------------------------------------- preferences that mask
+LOWEST = float(np.finfo(np.float32).min)
+
+
+def check_masked(s):
+    """The bound of Step.check with S, the scores' magnitude, taken over the keys that have weight and are not masked: masked scores that
+    tie differ by nothing, in fp32 as in fp64, and those below others by more than either can hold."""
+    torch.cuda.synchronize()
+    O = f64(s.O)
+    alpha, rho = f64(s.alpha), f64(s.rho)
+    for r in range(len(s.lens)):
+        a, n = int(s.offsets[r]), s.new[r]
+        want, _, A, S = orc.attend(f64(s.q[a:a + n]), f64(s.k[r]), f64(s.v[r]), s.lens[r] - n, s.mask, alpha, rho, s.pos[r], None, None)
+        for i in range(n):
+            for h in np.nonzero(s.mask)[0]:
+                x = np.array([alpha[h, j] + rho[h, s.pos[r][i] - j] for j in range(s.lens[r] - n + i + 1)])
+                x = x[(x - x.max() > -200) & (np.abs(x) < 1e6)]
+                S[i, h] = np.abs(x).max(initial=0.0)
+        rel = 2 * (s.D + 6) * S[..., None] * 2.0 ** -23 + 2.0 ** -20 + 2 * (s.lens[r] + 64) * 2.0 ** -23
+        bf = s.O.dtype == torch.bfloat16
+        tol = A * (rel + (2.0 ** -8 if bf else 2.0 ** -22)) + np.abs(want) * (2.0 ** -8 if bf else 2.0 ** -24)
+        bad = ~(np.abs(O[a:a + n] - want) <= tol)
+        assert not bad.any(), (r, np.argwhere(bad)[:5], O[a:a + n][bad][:5], want[bad][:5], tol[bad][:5])
+
+
+@pytest.mark.parametrize("low", [LOWEST, -3e38, -2.2e38, -1e38, -1e30, -1.1e30, -1.7e30, -2.9e30, -1e18, -1.3e18, 1e30, 1.3e30])
+@pytest.mark.parametrize("D,g,new,out", [(64, 1, 1, "bf16"), (128, 8, 1, "fp32"), (96, 8, 3, "bf16"), (64, 8, 40, "bf16"), (96, 8, 9, "bf16"), (128, 8, 5, "bf16"),
+                                         (128, 8, 40, "fp32")])
+def test_rows_whose_keys_are_masked_by_low_preferences(low, D, g, new, out):
+    """Key preferences at a value that masks (the lowest of the type, -1e30 and others): alone they are all alike, beside others they do not
+    count, and where they come first they leave nothing behind."""
+    s = Step([300 + new, 70 + new, new], [new] * 3, 8, g, D, 16, "page", range(8), out=out, seed=21)
+    s.alpha[0, :] = low                                     # every key
+    s.alpha[1, :100] = low                                  # padding in front
+    s.alpha[2, 20:] = low                                   # only the first keys count
+    s.alpha[3, :] = low
+    s.alpha[3, 40] = 0.5                                    # one key counts
+    s.alpha[4, ::2] = low
+    s.rho[5, 12:] = low                                     # a window
+    s.alpha[6, :50] = low                                   # two values that mask
+    s.alpha[6, 50:] = low / 2
+    s.rho[7, :] = low
+    s.call(saf.Context(0))
+    check_masked(s)
+
+
+@pytest.mark.parametrize("D,g,new", [(64, 1, 1), (128, 8, 3), (64, 8, 40), (128, 8, 40)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_rows_whose_low_preferences_are_split_over_blocks(D, g, new, out):
+    s = Step([5000 + new], [new], 8, g, D, 64, "page", range(8), out=out, seed=22)
+    s.alpha[0, :] = LOWEST
+    s.alpha[1, :4000] = LOWEST
+    s.alpha[2, 1000:] = LOWEST
+    s.alpha[3, :] = -1e30
+    s.alpha[4, :4500] = -1.3e30
+    s.alpha[5, 30:] = -1e30
+    s.alpha[6, :2500] = LOWEST
+    s.alpha[6, 2500:] = -2.5e38                             # (past the type's range in powers of two, both)
+    s.rho[7, :] = -1.7e30
+    s.call(saf.Context(0))
+    check_masked(s)
+
+
+@pytest.mark.parametrize("D,g,new", [(64, 1, 1), (128, 8, 3), (64, 8, 40), (96, 8, 40), (128, 8, 40)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_large_magnitude(D, g, new, out, sign):
+    """Queries and keys whose products are exact and large: 2^40 times small whole numbers that tie.  The largest take all."""
+    s = Step([150 + new, new], [new] * 2, 8, g, D, 16, "page", (), out=out, scale=0.125, seed=23)
+    rng = np.random.default_rng(24)
+    s.q.zero_()
+    s.q[..., 0] = 2.0 ** 20
+    for r in range(2):
+        j = np.arange(s.lens[r])
+        p, at = s.table[r][torch.from_numpy(j // 16).cuda()].long(), torch.from_numpy(j % 16).cuda()
+        c = torch.from_numpy(sign * rng.integers(3, 8, (s.lens[r], 8 // g))).cuda()
+        s.k[r].zero_()
+        s.k[r][..., 0] = c * 2.0 ** 20
+        s.kc[p, :, at] = s.k[r]
+    s.call(saf.Context(0))
+    torch.cuda.synchronize()
+    for r in range(2):
+        a, n = int(s.offsets[r]), new
+        want, lse, A, _ = orc.attend(f64(s.q[a:a + n]), f64(s.k[r]), f64(s.v[r]), s.lens[r] - n, s.mask, f64(s.alpha), f64(s.rho), s.pos[r], None, 0.125)
+        half = 2.0 ** -8 if out == "bf16" else 2.0 ** -22   # (equal weights: no rounding but in the sums and on the way out)
+        assert (np.abs(f64(s.O[a:a + n]) - want) <= (2.0 ** -20 + 2 * (s.lens[r] + 64) * 2.0 ** -23) * A + half * np.abs(want)).all()
+        assert (np.abs(f64(s.LSE[a:a + n]) - lse) <= np.abs(lse) * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("D,g,new,out", [(64, 1, 1, "fp32"), (96, 8, 3, "bf16"), (64, 8, 40, "bf16"), (128, 8, 40, "bf16")])
+def test_rows_whose_preferences_are_all_minus_infinity(D, g, new, out):
+    s = Step([300 + new, 70 + new], [new] * 2, 8, g, D, 16, "page", (0, 2, 5), out=out, seed=25)
+    s.alpha[0, :] = float("-inf")
+    s.alpha[2, :100] = float("-inf")
+    s.alpha[5, :], s.rho[5, :] = LOWEST, LOWEST             # (their sum in fp32)
+    s.call(saf.Context(0))
+    torch.cuda.synchronize()
+    total = 2 * new
+    assert not s.O[:total, 0].any() and not s.O[:total, 5].any()
+    for i, pos in enumerate(int(x) for p in s.pos for x in p):
+        assert bool(s.O[i, 2].any()) == (pos >= 100)        # (that head's first key with weight)
+    assert torch.isfinite(s.O).all() and not s.LSE[:total, [0, 2, 5]].any()
