@@ -355,7 +355,8 @@ int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, cons
  *                   Finite preferences count whatever their size; a key whose alpha + rho, a sum in fp32, is -inf has no weight.
  * A row that sees nothing, or nothing with weight, gives zeros.  NaN and infinities in slots that a row does not see do not reach it.
  *   Q, O: [N][H][D] by c->q_strides, o_strides; K and V pools; block_table, new_offsets, kv_lens as from saf_cache_plan (lengths beyond
- *   max_len and page numbers outside the pool are clamped, rows beyond max_new of a request are left as they are)
+ *   max_len and page numbers outside the pool are clamped; rows beyond max_new of a request are left as they are, and the others see
+ *   what they would without the bound, but for new tokens behind the 64th or without a row)
  *   positions [N] of the new tokens, or NULL: ctx + place (read for frozen heads only; values outside [0, Tp) are clamped)
  *   frozen_mask_host, alpha, rho as in saf_hybrid_attn_fwd (no logZ: the sum over the keys is formed here); H <= 1024
  *   LSE: device fp32 [N][H] or NULL: natural-log sum of exp of the scaled scores, 0 for frozen heads, -inf for a row of an

@@ -172,7 +172,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       next_unit<KT, ROWS>(p, u);
       continue;
     }
-    const int ctx = u.len - u.many, rows = min(ROWS, u.many * g - u.rt * ROWS);
+    const int ctx = u.ctx, rows = min(ROWS, u.many * g - u.rt * ROWS);
     const bool keys = has_keys(p, u.hk);
     // queries, as columns: column gid of each block of eight rows
     uint32_t q[NB][D / 16][2];

@@ -20,7 +20,8 @@ __device__ __forceinline__ float natural_lse(float m, float l) { return fmaf(m, 
 struct Unit {
   int start;                        // of the unit's first tile on the line
   int r, hk, rt;                    // request, cached head, row tile
-  int first, many, len;             // the request's first row, rows that are computed, tokens in its cache
+  int first, many, len;             // the request's first row, rows that are computed, tokens in its cache that rows may see
+  int ctx;                          // tokens that were cached before the step: place of the first new one
   int tiles, row_tiles, pitch;      // (pitch: places that a unit takes, 0: its tiles)
 };
 
@@ -28,9 +29,13 @@ __device__ __forceinline__ bool has_keys(const CacheAttnParams& p, int hk) { ret
 
 template <int KT, int ROWS>
 __device__ __forceinline__ void set_request(const CacheAttnParams& p, Unit& u, int first, int last, int len) {
+  // New tokens that no row can see, behind the 64th or the last row (nor more of them than that before the cache begins), are left out.
   u.first = min(max(first, 0), p.N);
-  u.many = min(max(min(last, p.N) - u.first, 0), p.max_new);
+  const int n = max(last, u.first) - u.first, there = min(n, p.N - u.first);
+  u.many = min(there, p.max_new);
   u.len = min(max(len, 0), p.max_len);
+  u.ctx = max(u.len - n, -64);
+  u.len = max(min(u.len, u.ctx + min(there, 64)), 0);
   u.row_tiles = ROWS <= 16 ? (u.many * p.kv_group + ROWS - 1) / ROWS : (u.many + p.tile_tokens - 1) / p.tile_tokens;
   u.tiles = max((u.len + KT - 1) / KT, 1);                    // (a request without keys still gets its zeros)
 }

@@ -103,6 +103,9 @@ __device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint
   return wild;
 }
 
+// New tokens of the unit's request whose keys rows may see (those that are not computed too); up to 64, and they have rows.
+__device__ __forceinline__ int new_keys(const CacheAttnParams& p, const Unit& w) { return min(w.len - w.ctx, p.N - w.first); }
+
 // Whether and how a unit's frozen rows go by bands; by a whole warp, the same for all.  A band serves a row whose position is at most 63 past the
 // unit's first, and a key whose position is at most 63 from its tile's first slot: a cached key's is its place; a new token's, whichever of the
 // request's it is, has to lie between the first new place and its own, as positions by place or by depth do.  (Out of line, once for both kinds of warps that ask: 24 trees 137 us, 141
@@ -118,12 +121,12 @@ __device__ __noinline__ BandPlan plan_band(const CacheAttnParams& p, const Unit&
     b.n_frozen += (p.frozen[hk >> 5] >> (hk & 31)) & 1;
   }
   if (b.n_frozen == 0) return b;
-  const int ctx = w.len - w.many, t0 = w.rt * p.tile_tokens, t1 = min(t0 + p.tile_tokens, w.many);
+  const int ctx = w.ctx, fresh = new_keys(p, w), t0 = w.rt * p.tile_tokens, t1 = min(t0 + p.tile_tokens, w.many);
   int lo = 0x7fffffff, hi = 0;
   bool near = ctx >= 0;
 #pragma unroll
   for (int c = threadIdx.x & 31; c < 64; c += 32) {
-    if (c >= w.many) continue;
+    if (c >= fresh) continue;
     const int x = p.positions ? min(max(p.positions[w.first + c], 0), p.Tp - 1) : max(ctx + c, 0);
     near &= x >= ctx && x <= ctx + c;
     if (c >= t0 && c < t1) {
@@ -332,7 +335,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     for (; ok && u.r < p.R && u.start < x1; next_unit<KT, ROWS>(p, u)) {
       const int tb = tile_at(u, x0), te = tile_at(u, x1);
       if (tb >= te) continue;
-      const int ctx = u.len - u.many;
+      const int ctx = u.ctx;
       const BandPlan b = plan_band(p, u);
       if (!b.fast) continue;
       for (int s = 0; s < 2 && ok; ++s) ok = mbar_wait_warp_compact(&band_empty[s], (used[s] & 1) ^ 1, wc, SITE_BAND_EMPTY);
@@ -393,14 +396,14 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       const int tb = range_s[k & 1][0], te = range_s[k & 1][1];
       if (te < 0) break;
       const Unit& w = work[k & 1];
-      const int ctx = w.len - w.many, rows = unit_rows<ROWS>(p, w.many, w.rt);
+      const int ctx = w.ctx, fresh = new_keys(p, w), rows = unit_rows<ROWS>(p, w.many, w.rt);
       const bool keys = has_keys(p, w.hk), there = tid < rows, idle = warp * 32 >= rows;
       int i, hg;
       row_at<ROWS>(p, w.many, w.rt, there ? tid : 0, i, hg);
       const int h = w.hk * g + hg, n = w.first + i;
       const bool frozen = (p.frozen[h >> 5] >> (h & 31)) & 1;
       unsigned long long mask = !there ? 0 : p.masks ? p.masks[n] : (2ull << i) - 1;
-      if (w.many < 64) mask &= (1ull << w.many) - 1;
+      if (fresh < 64) mask &= (1ull << fresh) - 1;
       if (keys) {
         // queries of ordinary rows, zeros elsewhere, as the swizzled tile that TMA would leave
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + static_cast<int64_t>(n) * p.q_strides[0] + h * p.q_strides[1];
@@ -414,7 +417,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         warp_arrive(&q_full);
       }
       if (tid == 0) wild_s = 0;
-      if (tid < w.many) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
+      if (tid < fresh) newpos[tid] = p.positions ? min(max(p.positions[w.first + tid], 0), max(p.Tp - 1, 0)) : max(ctx + tid, 0);
       named_bar_sync(6, 128);
       const BandPlan plan = plan_band(p, w);
       const bool fast = plan.fast;
@@ -425,7 +428,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       if (plan.n_frozen > 0) {
         pos = newpos[i];
         if (frozen && (p.positions || p.masks)) {            // (new tokens behind the row's position are not seen)
-          for (int c = 0; c < w.many; ++c)
+          for (int c = 0; c < fresh; ++c)
             if (newpos[c] > pos) mask &= ~(1ull << c);
         }
         int slot = 0;                                        // frozen heads of the group before this one
@@ -582,7 +585,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           tmem_ld32(t_s + 128 + f0, r);
           tmem_wait_ld();
           if (wild_s && there) {
-            for (int back = max(tb * KT - ctx, 0); back < w.many && ctx + back < min(te * KT, w.len); ++back) {
+            for (int back = max(tb * KT - ctx, 0); ctx + back < min(te * KT, w.len); ++back) {
               const int j = ctx + back;
               if (j < 0 || !((mask >> back) & 1)) continue;
               const int page = min(max(p.block_table[static_cast<int64_t>(w.r) * p.max_pages + j / p.page_size], 0), p.n_pages - 1);

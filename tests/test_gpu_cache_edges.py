@@ -160,3 +160,64 @@ def test_rows_whose_preferences_are_all_minus_infinity(D, g, new, out):
     for i, pos in enumerate(int(x) for p in s.pos for x in p):
         assert bool(s.O[i, 2].any()) == (pos >= 100)        # (that head's first key with weight)
     assert torch.isfinite(s.O).all() and not s.LSE[:total, [0, 2, 5]].any()
+
+
+# ------------------------------------------------------------------------------------------------------------------- rows that are not computed
+def check_first(s, many, known=None):
+    """The first `many` rows of each request against the oracle over all of its keys (`known`: new tokens of which keys are seen)."""
+    torch.cuda.synchronize()
+    bf = s.O.dtype == torch.bfloat16
+    for r in range(len(s.lens)):
+        a, n = int(s.offsets[r]), s.new[r]
+        m = min(many, n)
+        ctx, z = s.lens[r] - n, min(n, known or n)
+        sets = [x & ((1 << z) - 1) for x in s.sets[r][:z]] if s.tree else None
+        want, lse, A, S = orc.attend(f64(s.q[a:a + z]), f64(s.k[r][:ctx + z]), f64(s.v[r][:ctx + z]), ctx, s.mask, f64(s.alpha), f64(s.rho), s.pos[r][:z], sets, None)
+        rel = 2 * (s.D + 6) * S[..., None] * 2.0 ** -23 + 2.0 ** -20 + 2 * (s.lens[r] + 64) * 2.0 ** -23
+        tol = A * (rel + (2.0 ** -8 if bf else 2.0 ** -22)) + np.abs(want) * (2.0 ** -8 if bf else 2.0 ** -24)
+        bad = ~(np.abs(f64(s.O[a:a + z]) - want) <= tol)[:m]
+        assert not bad.any(), (r, np.argwhere(bad)[:5])
+        fin = np.isfinite(lse[:m])
+        assert np.array_equal(f64(s.LSE[a:a + m])[~fin], lse[:m][~fin])
+        assert (np.abs(f64(s.LSE[a:a + m]) - np.where(fin, lse[:m], 0)) <= (rel[..., 0] + np.abs(lse) * 2.0 ** -22)[:m])[fin].all()
+        assert (s.O[a + m:a + n] == 9.0).all() and (s.LSE[a + m:a + n] == 9.0).all()
+
+
+@pytest.mark.parametrize("D,g,max_new,out", [(64, 2, 2, "bf16"), (128, 4, 3, "fp32"), (64, 4, 33, "bf16"), (96, 2, 34, "bf16"), (128, 2, 20, "bf16")])
+@pytest.mark.parametrize("tree,positions", [(False, True), (False, False), (True, True)])
+def test_rows_of_requests_that_bring_more_than_the_bound(D, g, max_new, out, tree, positions):
+    """Rows up to the bound see what they see without it: the context, and of the new tokens their own."""
+    new = [max_new + 4, 50, max_new, max_new + 1, 2]
+    lens = [300 + new[0], 50, 64 + max_new, 17 + new[3], 90]
+    s = Step(lens, new, 2 * g, g, D, 16, "page", (0,), out=out, tree=tree, positions=positions, max_new=max_new, seed=31)
+    if tree:
+        rng = np.random.default_rng(32)                     # later tokens in the sets, those behind the bound too
+        s.sets = [[int(x) for x in rng.integers(0, 2 ** 63, n, dtype=np.uint64) & np.uint64((1 << n) - 1)] for n in new]
+        s.masks = torch.from_numpy(np.array([x for t in s.sets for x in t] + [0] * 2, dtype=np.uint64).view(np.int64)).cuda()
+    s.call(saf.Context(0))
+    check_first(s, max_new)
+
+
+@pytest.mark.parametrize("D,g,max_new", [(64, 2, 8), (128, 2, 64)])
+def test_rows_of_a_prompt_longer_than_a_set(D, g, max_new):
+    new = [200, 70, 65]
+    s = Step([200, 300 + 70, 1 + 65], new, 2 * g, g, D, 16, "page", (0,), max_new=max_new, seed=33)
+    s.call(saf.Context(0))
+    check_first(s, max_new)
+
+
+@pytest.mark.parametrize("D,g,new", [(64, 2, 6), (128, 4, 40)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_rows_of_a_request_that_ends_behind_the_last_row(D, g, new, tree):
+    """Offsets past N: the rows that there are see their context and the new tokens that have rows."""
+    s = Step([100 + new, 77 + new], [new, new], 2 * g, g, D, 16, "page", (0,), tree=tree, pad=0, seed=34)
+    if tree:
+        s.sets[1] = [(1 << new) - 1] * new
+        s.masks = torch.from_numpy(np.array([x for t in s.sets for x in t], dtype=np.uint64).view(np.int64)).cuda()
+    s.prob.N = new + 5
+    s.call(saf.Context(0))
+    torch.cuda.synchronize()
+    assert (s.O[new + 5:] == 9.0).all() and (s.LSE[new + 5:] == 9.0).all()
+    s.new, s.lens = [new, 5], [100 + new, 77 + 5]
+    s.k[1], s.v[1], s.pos[1], s.sets[1] = s.k[1][:82], s.v[1][:82], s.pos[1][:5], [x & 31 for x in s.sets[1][:5]]
+    check_first(s, new)
