@@ -214,7 +214,16 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
         rrow[b][e] = p.rho + static_cast<int64_t>(h) * p.Tp;
       }
     const bool any_frozen = __any_sync(0xffffffffu, any);
+    int from = ctx;                                            // first key that some row does not see
     if (any_frozen) {
+      int lowest = 0x7fffffff;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (frozen[b][e]) lowest = min(lowest, pos[b][e]);
+      lowest = __reduce_min_sync(0xffffffffu, lowest);
+      if (lowest < ctx) from = lowest + 1;
       // rows of ordinary heads look where the unit's first frozen row looks, so that their loads cost nothing
       const int first_row = __reduce_min_sync(0xffffffffu, first_frozen);
       const int at = u.rt * ROWS + first_row, i = by_group(p, at), h = u.hk * g + at - i * g, n = u.first + i;
@@ -274,7 +283,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     for (int t = t_begin; t < t_end; ++t) {
       const uint32_t ks_addr = ring_s + stage * STAGE, vs_addr = ks_addr + TILE;
       const int j0 = t * KT;
-      const bool tail = j0 + KT > ctx;
+      const bool tail = j0 + KT > ctx, unseen = j0 + KT > from;
       if (!mbar_wait_warp_compact(&full[warp][stage], phase, wc, 90)) {
         alive = false;
         break;
@@ -378,7 +387,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
               l[b][e] += x;
             }
         }
-      if (tail) {
+      if (unseen) {
         // values behind the last key are whatever the page held, and a value that some rows do not see may be NaN or infinite: both
         // are zeroed for the product, the second kind added by hand to the rows that see it
         bool wild = false;
@@ -459,7 +468,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             for (int i = 0; i < (EXACT ? 3 : 1); ++i) mma16816(o[b][f], a, w[b][i][0], w[b][i][1]);
         }
       }
-      if (tail) fence_proxy_async_smem();                     // (the tile may have been written to: before it is fetched over)
+      if (unseen) fence_proxy_async_smem();                    // (the tile may have been written to: before it is fetched over)
       __syncwarp();
       --ahead;
       if (++stage == stages) {

@@ -76,15 +76,15 @@ __device__ __noinline__ void slow_scores(const CacheAttnParams& p, const Unit& w
   tmem_wait_st();
 }
 
-// Values behind the last key are whatever was there, and those of new tokens, which not every row sees, may be NaN or infinite:
+// Values behind the last key are whatever was there, and those from key `from` on, which not every row sees, may be NaN or infinite:
 // both are zeroed for the product; true if there were any of the second kind (they are added to the rows that see them at the end).
 template <int D>
-__device__ __noinline__ bool clean_values(int br, int j0, int ctx, int len, uint32_t vs, int tid) {
+__device__ __noinline__ bool clean_values(int br, int j0, int from, int len, uint32_t vs, int tid) {
   constexpr int PANELS = Cfg<D>::PANELS;
   bool wild = false;
   for (int c = tid; c < Cfg<D>::TILE / 16; c += 128) {
     const int box = c / (8 * br * PANELS), j = j0 + box * br + ((c >> 3) & (br - 1));
-    if (j < ctx) continue;
+    if (j < from) continue;
     const uint32_t addr = vs + c * 16;
     uint32_t w[4];
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
@@ -421,6 +421,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       named_bar_sync(6, 128);
       const BandPlan plan = plan_band(p, w);
       const bool fast = plan.fast;
+      const int from = plan.n_frozen > 0 ? min(ctx, plan.pmin + 1) : ctx;   // first key that some row does not see
       bool any_frozen = false;
       uint32_t band_at = 0;                                  // this row's band: alpha of key 0
       int rho_at = 0;                                        // from there to rho of that key
@@ -563,9 +564,9 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           else ++band0;
         }
         if (!waited && !mbar_wait_warp_compact(&pv_done, (count & 1) ^ 1, wc, SITE_PV_DONE)) ok = false;   // (each phase is waited for in turn)
-        if (!plain) {
+        if ((t + 1) * KT > from) {
           if (!mbar_wait_warp_compact(&v_full[count % C::ST], (count / C::ST) & 1, wc, SITE_V_FULL)) ok = false;
-          if (clean_values<D>(p.box_rows, t * KT, ctx, w.len, smem_u32(smem) + C::OFF_V + (count % C::ST) * C::TILE, tid)) wild_s = 1;
+          if (clean_values<D>(p.box_rows, t * KT, from, w.len, smem_u32(smem) + C::OFF_V + (count % C::ST) * C::TILE, tid)) wild_s = 1;
           fence_proxy_async_smem();
         }
         tmem_wait_st();
@@ -585,9 +586,8 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           tmem_ld32(t_s + 128 + f0, r);
           tmem_wait_ld();
           if (wild_s && there) {
-            for (int back = max(tb * KT - ctx, 0); ctx + back < min(te * KT, w.len); ++back) {
-              const int j = ctx + back;
-              if (j < 0 || !((mask >> back) & 1)) continue;
+            for (int j = max(max(tb * KT, from), 0); j < min(te * KT, w.len); ++j) {
+              if (j < ctx ? frozen && j > pos : !((mask >> (j - ctx)) & 1)) continue;
               const int page = min(max(p.block_table[static_cast<int64_t>(w.r) * p.max_pages + j / p.page_size], 0), p.n_pages - 1);
               const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + page * p.v_strides[0] + w.hk * p.v_strides[1] + (j % p.page_size) * p.v_strides[2] + f0;
 #pragma unroll

@@ -221,3 +221,30 @@ def test_rows_of_a_request_that_ends_behind_the_last_row(D, g, new, tree):
     s.new, s.lens = [new, 5], [100 + new, 77 + 5]
     s.k[1], s.v[1], s.pos[1], s.sets[1] = s.k[1][:82], s.v[1][:82], s.pos[1][:5], [x & 31 for x in s.sets[1][:5]]
     check_first(s, new)
+
+
+# ------------------------------------------------------------------------------------------------------------------- values that are not finite
+@pytest.mark.parametrize("D,g,new", [(64, 1, 5), (96, 2, 7), (128, 4, 3), (64, 4, 40), (96, 2, 48), (128, 4, 40)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+def test_cached_values_behind_a_frozen_rows_position_do_not_reach_it(D, g, new, what):
+    ctx = 230
+    s = Step([ctx + new, 90 + new], [new] * 2, 2 * g, g, D, 16, "page", (0, g), tree=True, seed=41)
+    rng = np.random.default_rng(42)
+    place(s, [rng.integers(40, ctx + new, new), s.pos[1]])
+    context = saf.Context(0)
+    s.call(context)
+    s.check()
+    clean, lse = s.O.clone(), s.LSE.clone()
+    for hit in (45, 150, 229):                              # tiles of cached keys alone, and the one where the new tokens begin
+        s.vc[int(s.table[0, hit // 16]), :, hit % 16, 3] = what
+        s.call(context)
+        torch.cuda.synchronize()
+        for i in range(new):
+            for h in range(2 * g):
+                if s.mask[h] and s.pos[0][i] < hit:
+                    assert torch.equal(s.O[i, h], clean[i, h]), (i, h, hit)
+                else:
+                    assert not torch.isfinite(s.O[i, h, 3]), (i, h, hit)
+                    assert torch.isfinite(s.O[i, h, 4:]).all() and torch.isfinite(s.O[i, h, :3]).all()
+        assert torch.equal(s.O[new:2 * new], clean[new:2 * new]) and torch.equal(s.LSE, lse)
+        s.vc[int(s.table[0, hit // 16]), :, hit % 16, 3] = s.v[0][hit, :, 3]
