@@ -372,7 +372,8 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
 
 /* Device-side status of the most recent launches on this context: SAF_OK or SAF_ERR_DEVICE_TIMEOUT.
  * Synchronises the context's device status word with the host (blocks until the stream used by the
- * last call has drained).  `detail_out` (may be NULL) receives the raw word: site and CTA that gave up. */
+ * last call has drained).  `detail_out` (may be NULL) receives the raw word: site and CTA that gave up.  What a call that gave up
+ * wrote is undefined; later calls of saf_cache_attn, recorded ones too, are not affected by it. */
 int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out);
 
 /* Kernel timing for benchmarks.  With profiling enabled, every kernel the library launches is

@@ -91,6 +91,7 @@ struct saf_ctx {
   int fit_heads = 0;                       // of the last fit, and its per-head hand-over steps (nullptr: direct sums throughout)
   const int* fit_resume = nullptr;
   bool selftest_drop_load = false;         // SAF_SELFTEST_DROP_LOAD=1: see FwdParams::selftest_drop_load
+  bool selftest_drop_cached = false;       // the same for the first call of saf_cache_attn: see CacheAttnParams::selftest_drop_load
   DevBuf pat_consts, pat_ok, pat_avec, pat_wvec, pat_bandf, pat_bandb, pat_heads, pat_snap, pat_marks, vt_buf, dot_buf, pg_hlist, pg_delta, pg_items, pg_offsets, fit_buf, calib_tmp, cattn_buf, cattn_counters;
   std::vector<int> pg_hlist_host, pg_offsets_host;   // host copies of the pattern-gradient tables (upload sources)
   std::vector<PgItem> pg_items_host;
@@ -597,7 +598,7 @@ int saf_create(saf_ctx** out, int device) {
   }
   if (const char* e = std::getenv("SAF_DISABLE_TENSOR_PATTERN")) ctx->tensor_pattern = std::atoi(e) == 0;
   if (const char* e = std::getenv("SAF_FIT_DIRECT")) ctx->fit_direct = std::atoi(e) == 1;
-  if (const char* e = std::getenv("SAF_SELFTEST_DROP_LOAD")) ctx->selftest_drop_load = std::atoi(e) == 1;
+  if (const char* e = std::getenv("SAF_SELFTEST_DROP_LOAD")) ctx->selftest_drop_load = ctx->selftest_drop_cached = std::atoi(e) == 1;
   if (const char* e = std::getenv("SAF_FROZEN_WEIGHT_PCT")) {
     long v = std::atol(e);
     if (v > 0 && v <= 400) ctx->frozen_weight_pct = static_cast<int>(v);
@@ -1744,6 +1745,8 @@ int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* 
   f.counters = static_cast<int*>(ctx->cattn_counters.ptr);
   f.status = ctx->status_dev;
   f.wait_limit_ns = ctx->wait_limit_ns;
+  f.selftest_drop_load = ctx->selftest_drop_cached && ctx->wait_limit_ns <= 50000000ull ? 1 : 0;
+  ctx->selftest_drop_cached = false;
   CUtensorMap mk, mv;
   if ((rc = make_pool_map(ctx, &mv, v_cache, c, c->v_strides, form.halves_v, form.box_rows)) ||
       (rc = make_pool_map(ctx, &mk, ordinary ? k_cache : v_cache, c, ordinary ? c->k_strides : c->v_strides, form.halves_k, form.box_rows)))
@@ -1767,7 +1770,6 @@ int saf_last_device_status(saf_ctx* ctx, int32_t* detail_out) {
   if (detail_out) *detail_out = word;
   if (word != 0) {
     cudaMemset(ctx->status_dev, 0, sizeof(int));
-    ctx->cattn_counters.fresh = true;        // (blocks that gave up were not counted)
     return SAF_ERR_DEVICE_TIMEOUT;
   }
   return SAF_OK;

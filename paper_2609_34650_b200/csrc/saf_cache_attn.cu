@@ -69,7 +69,7 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   __shared__ int red[3][W], arrived_s[2], abort_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) abort_s = 0;
-  if (lane < stages) mbar_init(&full[warp][lane], 1);
+  if (lane < stages) mbar_init(&full[warp][lane], p.selftest_drop_load && blockIdx.x == 1 && warp + lane == 0 ? 2 : 1);
   if (threadIdx.x < 2) open_unit[threadIdx.x].start = -1;
   mbar_fence_init();
   if (threadIdx.x == 0) {
@@ -166,9 +166,15 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   uint32_t phase = 0;
   bool alive = true;
   Part lead{-1, 0, 0, 0, 0, 0};                              // a unit within the block whose parts this warp joins
-  while (alive && u.r < p.R && u.start < x1) {
+  // who joins a cut unit: the warp in whose run it begins, or, if it lies in several blocks, all of the block
+  auto is_open = [&]() { return u.start < b0 || u.start + u.tiles > b1; };
+  auto note_open = [&]() {                                   // (each warp of the unit writes the same)
+    if (lane == 0) open_unit[b0 >= u.start ? 0 : 1] = Part{u.start, u.start + u.tiles - 1, u.first, u.many, u.rt, u.hk};
+  };
+  while (u.r < p.R && u.start < x1) {
     const int t_begin = tile_at(u, x0), t_end = tile_at(u, x1);
-    if (t_begin >= t_end) {
+    if (t_begin >= t_end || !alive) {                        // (given up: what is left of the run is still reported, so that the counters end at zero)
+      if (t_begin < t_end && is_open()) note_open();
       next_unit<KT, ROWS>(p, u);
       continue;
     }
@@ -483,7 +489,6 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
-    const Part me{u.start, u.start + u.tiles - 1, u.first, u.many, u.rt, u.hk};
     if (!alive) {
       // given up: the copies in flight end before the block does (a bounded wait again), nothing is joined
       for (; ahead > 0; --ahead) {
@@ -494,7 +499,9 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
           phase ^= 1;
         }
       }
-    } else if (t_begin == 0 && t_end == u.tiles) {
+      continue;
+    }
+    if (t_begin == 0 && t_end == u.tiles) {
       // pairs of lanes exchange, the one taking the even row, the other the odd one, two features each
       const int odd = gid & 1;
 #pragma unroll
@@ -535,12 +542,8 @@ saf_cache_attn_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
             }
           }
         }
-      // who joins: the warp in whose run the unit begins, or, if it lies in several blocks, all of the block
-      if (me.start < b0 || me.last >= b1) {
-        if (lane == 0) open_unit[b0 >= me.start ? 0 : 1] = me;  // (each warp of the unit writes the same)
-      } else if (t_begin == 0) {
-        lead = me;
-      }
+      if (is_open()) note_open();
+      else if (t_begin == 0) lead = Part{u.start, u.start + u.tiles - 1, u.first, u.many, u.rt, u.hk};
     }
     next_unit<KT, ROWS>(p, u);
   }

@@ -160,7 +160,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], q_full, s_full[2], p_full, pv_done, o_free, band_full[2], band_empty[2];
   __shared__ Part open_unit[2];                              // units that go on in other blocks: the run's first, its last
-  __shared__ Unit work[2];                                   // what the compute warps are at, in turn
+  __shared__ Unit work[3];                                   // what the compute warps are at, in turn; the run's first
   __shared__ Cut cut_s;
   __shared__ int red[3][W], arrived_s[2], range_s[2][2], abort_s, wild_s;
   __shared__ uint32_t tmem_slot;
@@ -181,7 +181,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     for (int s = 0; s < C::ST; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&k_empty[s], 1);
-      mbar_init(&v_full[s], 1);
+      mbar_init(&v_full[s], p.selftest_drop_load && blockIdx.x == 1 && s == 0 ? 2 : 1);
       mbar_init(&v_empty[s], 1);
     }
     mbar_init(&q_full, 4);                                   // (one arrival per compute warp)
@@ -210,7 +210,7 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
     place_run<KT, ROWS, W, 1, SINGLE_TILES>(p, smem, red, 0, cut, x0, x1, u);
     if (tid == 0) {
       cut_s = cut;
-      work[1] = u;
+      work[1] = work[2] = u;
     }
   }
   __syncthreads();                                           // the sums have been read: tiles may be fetched over them
@@ -647,8 +647,15 @@ saf_cache_wide_kernel(const __grid_constant__ CUtensorMap mk, const __grid_const
   // ------------------------------------------------------------------ teardown; then units that lie in several blocks
   __syncwarp();
   if (abort_s) {
-    // a wait gave up: copies and MMAs in flight land before the block's memory is released
+    // a wait gave up: copies and MMAs in flight land before the block's memory is released, and what it did not come to is reported
+    // all the same, so that the counters end at zero
     for (int k = 0; k < 64; ++k) __nanosleep(20000);
+    if (tid == 0 && x0 < x1) {
+      for (Unit v = work[2]; v.r < p.R && v.start < x1; next_unit<KT, ROWS>(p, v)) {
+        const int tb = tile_at(v, x0), te = tile_at(v, x1);
+        if (tb < te && te - tb < v.tiles) open_unit[x0 >= v.start ? 0 : 1] = Part{v.start, v.start + v.tiles - 1, v.first, v.many, v.rt, v.hk};
+      }
+    }
   }
   tc_fence_before();
   __syncthreads();

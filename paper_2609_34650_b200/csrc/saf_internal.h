@@ -339,6 +339,9 @@ struct CacheAttnParams {
   int stages, parts_in_smem;        // set by the launcher
   int* status;
   unsigned long long wait_limit_ns;
+  // Self-test of the give-up path (0 in normal use): block 1 waits for one arrival more than its first tile makes.  Set in the first call of a
+  // context that was created with SAF_SELFTEST_DROP_LOAD, and only with a wait limit of at most 50 ms.
+  int selftest_drop_load;
   uint32_t frozen[CACHE_MAX_HEADS / 32];     // bit per query head
   uint32_t with_keys[CACHE_MAX_HEADS / 32];  // bit per cached head: some query head of its group is ordinary
 };

@@ -248,3 +248,35 @@ def test_cached_values_behind_a_frozen_rows_position_do_not_reach_it(D, g, new, 
                     assert torch.isfinite(s.O[i, h, 4:]).all() and torch.isfinite(s.O[i, h, :3]).all()
         assert torch.equal(s.O[new:2 * new], clean[new:2 * new]) and torch.equal(s.LSE, lse)
         s.vc[int(s.table[0, hit // 16]), :, hit % 16, 3] = s.v[0][hit, :, 3]
+
+
+# ------------------------------------------------------------------------------------------------------------------- waits that run out
+# (the last of each pair: on 148 SMs block 1, or its first warp, holds the end of one unit and the beginning of the next)
+@pytest.mark.parametrize("D,g,new,lens", [(64, 1, 1, [9000]), (64, 1, 1, [790, 9000]), (128, 4, 3, [5000, 3000]), (128, 4, 3, [270, 9000]),
+                                          (64, 4, 33, [9000]), (64, 4, 33, [890, 890, 9000]), (128, 4, 40, [4000, 3000]), (128, 4, 33, [890, 890, 9000])])
+def test_a_wait_that_runs_out_leaves_recorded_steps_whole(monkeypatch, D, g, new, lens):
+    """The context's first attention call leaves out one copy of a tile (a host-side switch, off by default), so that waits reach their limit
+    (20 ms here) in a block that holds parts of cut units.  The call is reported; a step recorded before the report is right."""
+    monkeypatch.setenv("SAF_WAIT_LIMIT_MS", "20")
+    monkeypatch.setenv("SAF_SELFTEST_DROP_LOAD", "1")
+    ctx = saf.Context(0)
+    monkeypatch.delenv("SAF_SELFTEST_DROP_LOAD")
+    monkeypatch.delenv("SAF_WAIT_LIMIT_MS")
+    s = Step(lens, [new] * len(lens), 2 * g, g, D, 16, "page", (0,), tree=True, seed=51)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.call(ctx)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        s.call(ctx)
+    code, detail = ctx.saf_last_device_status()
+    assert code == saf.SAF_ERR_DEVICE_TIMEOUT and (detail >> 24) & 0xFF == 1, (code, hex(detail))
+    assert (detail >> 16) & 0xFF in (90, *range(111, 122)) and detail & 0xFFFF == 1, hex(detail)
+    for _ in range(3):
+        s.O.fill_(9.0), s.LSE.fill_(9.0), s.q.normal_(), s.vc.copy_(s.vc.roll(1, 3)), s.v.__setitem__(slice(None), [x.roll(1, 2) for x in s.v])
+        torch.cuda.synchronize()
+        graph.replay()
+        s.check()
+    assert ctx.saf_last_device_status()[0] == saf.SAF_OK
