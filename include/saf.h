@@ -303,7 +303,8 @@ typedef struct {
   int32_t Tp;                  /* row length of alpha and rho; >= max_len where heads are frozen */
   int32_t max_len;             /* saf_cache_attn: no request's cache holds more tokens, new ones included; <= max_pages * page_size */
   int32_t max_new;             /* saf_cache_attn: no request brings more new tokens; 1 .. 64 */
-  int32_t o_dtype;             /* of O: SAF_BF16 or SAF_F32 */
+  int32_t o_dtype;             /* of O: SAF_BF16 or SAF_F32; it chooses the weights' precision too: rounded to bf16 for their product with the
+                                  values where O is bf16 (as in saf_hybrid_attn_fwd), 24 bits where it is fp32 */
   float softmax_scale;         /* <= 0 selects 1/sqrt(D) */
   int32_t reserved;            /* 0 */
   int64_t q_strides[2], o_strides[2];    /* elements: row, head */
@@ -363,6 +364,10 @@ int saf_cache_append(saf_ctx* ctx, const saf_cache* c, const saf_rotary* r, cons
  *   ordinary head that sees nothing
  * Q rows of frozen heads are never read, nor keys where all heads of a group are frozen.  D in {64, 96, 128}; max_len <= 2^31 - 256; R * (H / kv_group) *
  * ceil(max_len / 16) * ceil(max_new * kv_group / 8) < 2^31 (SAF_ERR_UNSUPPORTED beyond what the kernels' tiles reach, which is no less).
+ * Every key and value is read once for each 128 rows of a group (new tokens times kv_group), or for each 16 where max_new * kv_group * D < 4096, O is
+ * fp32 or kv_group > 128: the kernel goes by max_new, not by a step's rows, so record one-token steps with max_new = 1.
+ * The context keeps a workspace of 39 MB (148 SMs) for this call, whatever its sizes.  Once a drafted tree is verified, moving the accepted
+ * path's keys and values to the slots behind the context is the caller's.
  * Results do not vary from run to run.  One launch; recordable after one warm-up call with the same kv_group, D, max_new and o_dtype, and
  * recorded calls stay good when calls of other sizes follow in the context. */
 int saf_cache_attn(saf_ctx* ctx, const saf_cache* c, const void* Q, const void* k_cache, const void* v_cache,

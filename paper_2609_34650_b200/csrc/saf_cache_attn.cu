@@ -3,7 +3,7 @@
 //   O_i = sum_j e^{s_ij} V_j / sum_j e^{s_ij} over the keys j that row i sees; s_ij = scale q_i k_j (ordinary head) or
 //   alpha(p_j) + rho(p_i - p_j) (frozen head), running maximum and sum in fp32, in powers of 16.
 //
-// Every key and value is read once for all rows that share it, so DRAM bounds the call unless it is a short one.  A unit is one request,
+// Every key and value is read once for up to 16 rows that share it, so DRAM bounds a step of few rows unless it is a short one.  A unit is one request,
 // one cached head and up to 8 or 16 of its rows (new token, query head of the group); its keys come in tiles of 4 KB, 32 keys at
 // head dimension 64 and 16 above.  The units' tiles, laid end to end, are cut into equal runs, one for each warp of the grid: no run is longer than
 // another whatever the lengths are, and a single long request fills the GPU like many short ones.  A warp streams its run on its
@@ -620,8 +620,9 @@ CacheAttnForm cache_attn_form(int max_new, int kv_group, int D, int page_size, i
   const int rows = max_new * kv_group;
   // Units of 128 rows from 32 rows at head dimension 128, 43 at 96 and 64 at 64 on, where the two cross (us, this form / the wide one, 24 trees
   // on up to 8192 cached tokens, head dimension 128: 20 rows 95 / 122, 32 rows 131 / 124, 64 rows 225 / 137; 64: 48 rows 56 / 67, 64 rows
-  // 70 / 67; 8 chains at 96: 32 rows 72 / 77, 48 rows 99 / 82).  fp32 output needs weights of 24 bits, three terms of which the wide
-  // form's TMEM has no room for.
+  // 70 / 67; 8 chains at 96: 32 rows 72 / 77, 48 rows 99 / 82).  The rule goes by the bound on new tokens, which the launch knows, not by the rows
+  // that a step turns out to have.  fp32 output needs weights of 24 bits, three terms: at head dimension 128 the wide form's two blocks an SM leave
+  // no TMEM columns for them; at 96 and 64, where 32 and 64 are free, it has not been written.
   if (rows * D >= 4096 && kv_group <= 128 && !o_f32) return cache_wide_form(max_new, kv_group, D, page_size, max_len);
   CacheAttnForm f;
   f.wide = false;

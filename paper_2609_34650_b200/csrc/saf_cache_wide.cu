@@ -14,7 +14,7 @@
 // copied in ahead: 64 preferences of keys and 192 of distances for each of up to FZ frozen heads (up to twice as many
 // in one place instead of two); with more of them, or positions that are not near the tokens' places, they take them from global memory.
 //
-// 24 trees of up to 32 tokens on up to 8192 cached ones, 32 heads on 8, a third of them frozen: 135 us = 3.1 TB/s, 107 us without frozen
+// 24 trees of up to 32 tokens on up to 8192 cached ones, 32 heads on 8, a third of them frozen: 137 us = 3.1 TB/s, 107 us without frozen
 // heads.  In the second a tile and block takes 2740 clk, DRAM's rate for two blocks; the rest is the units' ends (12000 clk until the first
 // scores, behind loads already in flight, 9000 for the last product and the part) and the joins (25000).
 #include "saf_cache_attn.cuh"
